@@ -94,7 +94,10 @@ typedef enum {
   SAS_OP_DECODE_SELECT = 5, /* sas_decode_select: batch, seq_len = max context (tokens) */
   SAS_OP_ATTENTION_BACKWARD = 6, /* sas_attention_backward: batch, seq_len */
   SAS_OP_SELECTOR_BACKWARD = 7,  /* sas_selector_backward: batch, seq_len */
-  SAS_OP_SELECTION_STATS = 8     /* sas_selection_stats: batch, seq_len */
+  SAS_OP_SELECTION_STATS = 8,    /* sas_selection_stats: batch, seq_len */
+  SAS_OP_QK_BACKWARD = 9,        /* sas_qk_norm_rope_backward: batch = rows, seq_len ignored */
+  SAS_OP_ATTENTION_CHUNK = 10,   /* sas_attention_chunk: batch = sequences, seq_len = rows */
+  SAS_OP_VERIFY_DRAFTS = 11      /* sas_verify_drafts: batch = sequences, seq_len ignored (cfg is not read) */
 } sas_op;
 
 typedef struct {
@@ -490,6 +493,160 @@ sas_status sas_lm_head_argmax(const sas_config* cfg, int32_t batch, const void* 
                               const void* gamma, const void* w_lm, int32_t vocab,
                               float* logits, int32_t* tokens,
                               void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Chunks of new tokens over the paged cache ----------------------------
+ * A chunk brings any number of new tokens to each of `batch` sequences (at most
+ * 4096) whose earlier tokens are cached: pieces of long prompts, one generated
+ * token, a few drafted ones, or none.  The new tokens of all sequences are the
+ * rows of [rows, ...] arrays, sequence i's at row_start[i] .. row_start[i+1] - 1
+ * in order of their positions ctx_len[i] .. kv_len[i] - 1.  Rows at and after
+ * row_start[batch] are padding (a captured call has a fixed row count): their
+ * attention outputs are left as they were.  Lengths and offsets are DEVICE
+ * memory: the calls never wait for them, and contents that break the rules give
+ * unspecified (but in-bounds) results. */
+
+/* Requests of sas_plan_chunk, all DEVICE int32.
+ *  ctx_len, new_len [b]  cached tokens, tokens of the chunk (negative = 0)
+ *  pages_held [b]        leading entries of the sequence's block-table row that
+ *                        are its pages
+ *  free_pages [free_capacity], free_count [1]: a stack of free page ids, its top
+ *                        at free_pages[free_count - 1] */
+typedef struct {
+  const int32_t* ctx_len;
+  const int32_t* new_len;
+  const int32_t* pages_held;
+  const int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t free_capacity;
+} sas_plan_in;
+
+/* Outputs of sas_plan_chunk, all DEVICE and required; none may be an input.
+ *  row_start [b+1]  rows of the sequences; tokens past `rows` have no row
+ *  kv_len [b]       ctx_len + new_len
+ *  seq, pos [rows]  the row's sequence and position, -1 in padding rows
+ *  slot [rows] int64  page * page_size + offset of the row's key and value in the
+ *                   pool, -1 where the position has no page, and in padding rows
+ *  pages_held [b]   with the pages that were taken
+ *  free_count [1]   what is left of the stack (free_pages is not written)
+ *  missing [1]      pages that were wanted and not there */
+typedef struct {
+  int32_t* row_start;
+  int32_t* kv_len;
+  int32_t* seq;
+  int32_t* pos;
+  int64_t* slot;
+  int32_t* pages_held;
+  int32_t* free_count;
+  int32_t* missing;
+} sas_plan_out;
+
+/* Pages and slots of a chunk.  Each sequence with new tokens takes the pages that
+ * its positions need beyond those it holds off the top of the stack, the sequences
+ * in order, each page into the next entry of its row of cache->block_table (the
+ * other entries are left as they are).  When the stack runs out, the entries
+ * become -1 (unmapped) and are counted in `missing`; positions past
+ * max_pages_per_seq have no page.  Reads block_table, num_pages, page_size (a
+ * power of two up to 128) and max_pages_per_seq of the cache only. */
+sas_status sas_plan_chunk(int32_t batch, int32_t rows, const sas_plan_in* in, const sas_paged_kv* cache,
+                          const sas_plan_out* out, void* stream);
+
+/* Norm and rotation of query and key heads.
+ *  gain_q, gain_k [dh]  RMSNorm gains of every query / key head (eps cfg->rms_eps,
+ *                   over the head's dh values); NULL = no norm
+ *  pos [axes, rows] int32 DEVICE: positions along 1 to 3 axes (time, height,
+ *                   width of image and video tokens)
+ *  section [axes]   rotary pairs (i, i + dh/2) that turn by each axis, pairs in
+ *                   order, dh/2 together; pair i turns by
+ *                   pos[axis] * rope_base^(-2i/dh) */
+typedef struct {
+  const void* gain_q;
+  const void* gain_k;
+  const int32_t* pos;
+  int32_t axes;
+  int32_t section[3];
+} sas_rotary;
+
+/* Rows of query, key and value heads: q [rows, H, dh], k, v [rows, Hkv, dh] with
+ * q_stride .. elements from row to row (0 = contiguous; otherwise a multiple of 16
+ * bytes), such as the columns of one packed projection. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+} sas_qkv;
+
+/* q_out [rows, H, dh], k_out [rows, Hkv, dh] (contiguous) = the heads of in->q and
+ * in->k normed and rotated, computed in fp32 (angles in fp64) and rounded once.
+ * in->v is not read.  q_out may be in->q itself, and k_out in->k, when those are
+ * contiguous; other overlaps are not allowed. */
+sas_status sas_qk_norm_rope(const sas_config* cfg, int32_t rows, const sas_rotary* rot, const sas_qkv* in,
+                            void* q_out, void* k_out, void* stream);
+
+/* Its backward: d_q_out [rows, H, dh], d_k_out [rows, Hkv, dh] (contiguous) -> dq, dk
+ * (contiguous, activation dtype) and dgain_q, dgain_k [dh] fp32 (each required
+ * exactly when its gain is given; summed over rows and heads, the same bits
+ * every time).  ws: sas_workspace_size(cfg, SAS_OP_QK_BACKWARD, rows, 0). */
+sas_status sas_qk_norm_rope_backward(const sas_config* cfg, int32_t rows, const sas_rotary* rot, const sas_qkv* in,
+                                     const void* d_q_out, const void* d_k_out, void* dq, void* dk, float* dgain_q,
+                                     float* dgain_k, void* ws, size_t ws_bytes, void* stream);
+
+/* A chunk's heads into the cache: q_out as sas_qk_norm_rope; the normed and
+ * rotated k and v as it is go to the pages at slot [rows] (int64 DEVICE; a slot
+ * outside the pool drops the row's key and value; of two rows with one slot
+ * either may stay); then the summaries of the blocks that positions
+ * ctx_len[i] .. kv_len[i] - 1 complete are written to cache->k_summary (mean of
+ * the block's keys in the pages, projected by w_gk [Hkv, dh, dh] when given).
+ * q_out may be in->q itself when that is contiguous. */
+sas_status sas_cache_append(const sas_config* cfg, int32_t batch, int32_t rows, const sas_rotary* rot,
+                            const sas_qkv* in, const int64_t* slot, const int32_t* ctx_len, const int32_t* kv_len,
+                            const void* w_gk, const sas_paged_kv* cache, void* q_out, void* stream);
+
+/* Causal attention of the chunk's queries over the cache, the chunk's own keys
+ * (appended before) among them: row j of sequence i's m rows is at position
+ * t = kv_len[i] - m + j and attends every mapped position up to t (the dense
+ * prefill of Sec. 5.1 over a cache; cfg->mode is not read).
+ * q, o [rows, H, dh]; lse [rows, H] fp32 or NULL.  A row that attends nothing
+ * gives o = 0, lse = -inf.  H / Hkv <= 128; the block table covers at most 2^30
+ * positions.  ws: sas_workspace_size(cfg, SAS_OP_ATTENTION_CHUNK, batch, rows),
+ * of which all but the last 69 MiB (fewer for dh = 64), where parts of divided
+ * work are joined, is needed. */
+sas_status sas_attention_chunk(const sas_config* cfg, int32_t batch, int32_t rows, const void* q,
+                               const int32_t* row_start, const int32_t* kv_len, const sas_paged_kv* cache, void* o,
+                               float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Inputs of sas_verify_drafts, all DEVICE.  Sequence i drafted m = draft_start[i+1]
+ * - draft_start[i] tokens (0 .. max_draft), `rows` in all.
+ *  target [rows + b, vocab] fp32  the target's probabilities: for each sequence
+ *                   the m positions of its drafted tokens and the one after them
+ *                   (row draft_start[i] + i + j)
+ *  draft [rows, vocab] fp32 or NULL  the probabilities that the drafted tokens
+ *                   were drawn from; NULL = drafted without a distribution
+ *                   (probability 1 on the drafted token)
+ *  tokens [rows] int32 (a token outside the vocabulary is not accepted)
+ *  u_accept [rows], u_sample [b] fp32  uniform numbers in [0, 1) */
+typedef struct {
+  const float* target;
+  const float* draft;
+  const int32_t* tokens;
+  const int32_t* draft_start;
+  const float* u_accept;
+  const float* u_sample;
+} sas_verify_in;
+
+/* Speculative verification: drafted tokens are accepted in order while
+ * u_accept q(x) < p(x); then one token is drawn by u_sample from max(p - q, 0)
+ * normalized at the first that was not accepted (from p itself if nothing is
+ * left of it), or from p after the last: of the tokens of any weight the lowest
+ * whose cumulated weight exceeds u_sample times the sum (the last of them if none
+ * does; -1 if all weights are zero).  Products, differences and sums are fp64; weights that are negative
+ * or NaN count as zero.
+ * out_tokens [b, max_draft + 1] int32: the accepted tokens, the drawn one, -1;
+ * accepted [b] int32.  ws: sas_workspace_size(NULL, SAS_OP_VERIFY_DRAFTS, batch, 0). */
+sas_status sas_verify_drafts(int32_t batch, int32_t rows, int32_t vocab, int32_t max_draft, const sas_verify_in* in,
+                             int32_t* out_tokens, int32_t* accepted, void* ws, size_t ws_bytes, void* stream);
 
 /* Message describing the last non-OK status on this thread ("" if none). */
 const char* sas_last_error(void);

@@ -2,6 +2,7 @@
 // kernel sequence of every entry point.  No allocation happens here; all
 // scratch comes from the caller's workspace.
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 
@@ -721,6 +722,107 @@ bool packed_layout(const sas_config* c, PackedLayout& L) {
   return true;
 }
 
+// ---- chunks of new tokens ----
+
+float* carve_qk_backward(Carve& cv, const sas_config* c) {
+  return (float*)cv.take((size_t)QK_BWD_GROUPS * 2 * c->head_dim * 4);
+}
+
+size_t verify_part_bytes(int b) { return (size_t)b * VERIFY_PIECES * 2 * sizeof(double); }
+
+struct ChunkWs {
+  int32_t* head;
+  int32_t* job_base;
+  int2* seq_parts;
+  size_t need;  // bytes up to here; the parts may be fewer
+  float* part;
+  long long part_slots;
+};
+size_t chunk_part_bytes(const sas_config* c) { return (size_t)128 * (c->head_dim + 2) * 4; }
+ChunkWs carve_chunk(Carve& cv, size_t total, const sas_config* c, int b) {
+  ChunkWs w;
+  w.head = (int32_t*)cv.take(64);
+  w.job_base = (int32_t*)cv.take((size_t)b * 4);
+  w.seq_parts = (int2*)cv.take((size_t)b * 8);
+  w.need = cv.off;
+  w.part_slots = CHUNK_PART_SLOTS;
+  w.part = (float*)cv.take_some(total, chunk_part_bytes(c), w.part_slots);
+  return w;
+}
+
+sas_status check_chunk(int32_t batch, int32_t rows) {
+  if (batch <= 0 || rows <= 0)
+    return fail(SAS_ERR_INVALID_ARGUMENT, "batch %d and rows %d must be positive", batch, rows);
+  if (batch > CHUNK_MAX_SEQS)
+    return fail(SAS_ERR_UNSUPPORTED, "batch %d (supported: <= %d sequences)", batch, CHUNK_MAX_SEQS);
+  return SAS_OK;
+}
+
+// Checks the rows, heads and rotation of a norm/rotation call and fills its arguments.
+sas_status qk_args(const sas_config* c, int32_t rows, const sas_rotary* rot, const sas_qkv* in, bool with_v, QkArgs& a) {
+  SAS_TRY(check_config(c, false));
+  if (!(c->rms_eps >= 0.f)) return fail(SAS_ERR_INVALID_ARGUMENT, "rms_eps must be >= 0");
+  if (!(c->rope_base > 0.f)) return fail(SAS_ERR_INVALID_ARGUMENT, "rope_base must be > 0");
+  if (rows <= 0) return fail(SAS_ERR_INVALID_ARGUMENT, "rows %d must be positive", rows);
+  if ((long long)rows * (c->n_heads + 2ll * c->n_kv_heads) > INT32_MAX)
+    return fail(SAS_ERR_UNSUPPORTED, "%d rows of %d/%d heads (supported: fewer than 2^31 heads)", rows, c->n_heads,
+                c->n_kv_heads);
+  if (!rot || !in) return fail(SAS_ERR_INVALID_ARGUMENT, "rot/in is NULL");
+  SAS_TRY(check_ptr(rot->gain_q, "rot.gain_q", false));
+  SAS_TRY(check_ptr(rot->gain_k, "rot.gain_k", false));
+  SAS_TRY(check_ptr(rot->pos, "rot.pos", true));
+  if (rot->axes < 1 || rot->axes > 3) return fail(SAS_ERR_INVALID_ARGUMENT, "axes %d (1..3)", rot->axes);
+  long long pairs = 0;
+  for (int i = 0; i < rot->axes; ++i) {
+    if (rot->section[i] < 0) return fail(SAS_ERR_INVALID_ARGUMENT, "section[%d] is negative", i);
+    pairs += rot->section[i];
+  }
+  if (pairs != c->head_dim / 2)
+    return fail(SAS_ERR_INVALID_ARGUMENT, "the sections hold %lld rotary pairs, head_dim %d has %d", pairs,
+                c->head_dim, c->head_dim / 2);
+  SAS_TRY(check_ptr(in->q, "in.q", true));
+  SAS_TRY(check_ptr(in->k, "in.k", true));
+  SAS_TRY(check_ptr(in->v, "in.v", with_v));
+  const long long unit = 16 / (long long)act_bytes(c);
+  auto stride = [&](int64_t s, int heads, const char* name, long long& out) {
+    const long long width = (long long)heads * c->head_dim;
+    out = s ? s : width;
+    if (out < width || out % unit || out > INT64_MAX / 16 / rows)
+      return fail(SAS_ERR_INVALID_ARGUMENT, "%s %lld (at least %lld, a multiple of %lld elements)", name, (long long)s,
+                  width, unit);
+    return SAS_OK;
+  };
+  a = {};
+  SAS_TRY(stride(in->q_stride, c->n_heads, "q_stride", a.qs));
+  SAS_TRY(stride(in->k_stride, c->n_kv_heads, "k_stride", a.ks));
+  if (with_v) SAS_TRY(stride(in->v_stride, c->n_kv_heads, "v_stride", a.vs));
+  a.rows = rows;
+  a.H = c->n_heads;
+  a.Hkv = c->n_kv_heads;
+  a.dh = c->head_dim;
+  a.axes = rot->axes;
+  a.sec0 = rot->section[0];
+  a.sec1 = rot->axes > 1 ? rot->section[1] : 0;
+  a.eps = c->rms_eps;
+  a.log2_base = log2((double)c->rope_base);
+  a.q = in->q;
+  a.k = in->k;
+  a.v = with_v ? in->v : nullptr;
+  a.gain_q = rot->gain_q;
+  a.gain_k = rot->gain_k;
+  a.pos = rot->pos;
+  return SAS_OK;
+}
+
+// an output may be its contiguous input itself
+sas_status check_in_place(const void* in, long long stride, int heads, int dh, const void* out, const char* name) {
+  if (out == in && stride != (long long)heads * dh)
+    return fail(SAS_ERR_INVALID_ARGUMENT, "%s is its input, whose rows are not contiguous", name);
+  return SAS_OK;
+}
+
+int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
+
 }  // namespace
 
 namespace sas {
@@ -764,7 +866,7 @@ int32_t sas_profiler_record(int32_t i, const char** name, float* ms) {
 }
 
 size_t sas_workspace_size(const sas_config* c, int32_t op, int32_t batch, int32_t seq_len) {
-  if (!c || batch <= 0) return 0;
+  if (batch <= 0 || (!c && op != SAS_OP_VERIFY_DRAFTS)) return 0;
   Carve cv(nullptr);
   switch (op) {
     case SAS_OP_ATTENTION:
@@ -805,6 +907,17 @@ size_t sas_workspace_size(const sas_config* c, int32_t op, int32_t batch, int32_
     case SAS_OP_LM_HEAD:
       if (seq_len <= 0 || !c || (c->dtype != SAS_F32 && c->dtype != SAS_BF16) || c->d_model <= 0) return 0;
       carve_lm(cv, c, batch, seq_len);
+      break;
+    case SAS_OP_QK_BACKWARD:
+      if (check_config(c, false) != SAS_OK) return 0;
+      carve_qk_backward(cv, c);
+      break;
+    case SAS_OP_ATTENTION_CHUNK:
+      if (seq_len <= 0 || batch > CHUNK_MAX_SEQS || check_config(c, false) != SAS_OK) return 0;
+      carve_chunk(cv, SIZE_MAX, c, batch);
+      break;
+    case SAS_OP_VERIFY_DRAFTS:
+      cv.take(verify_part_bytes(batch));
       break;
     default:
       return 0;
@@ -1521,6 +1634,243 @@ sas_status sas_lm_head_argmax(const sas_config* c, int32_t batch, const void* h,
     Timed tm("argmax", s);
     HIP_TRY(launch_argmax(lg, batch, vocab, lw.pv, lw.pi, ARGMAX_SLICES, tokens, s), "argmax");
   }
+  return SAS_OK;
+}
+
+sas_status sas_plan_chunk(int32_t batch, int32_t rows, const sas_plan_in* in, const sas_paged_kv* cache,
+                          const sas_plan_out* out, void* stream) {
+  SAS_TRY(check_chunk(batch, rows));
+  if (!in || !out || !cache) return fail(SAS_ERR_INVALID_ARGUMENT, "in/cache/out is NULL");
+  const int32_t* ins[] = {in->ctx_len, in->new_len, in->pages_held, in->free_pages, in->free_count};
+  const char* in_names[] = {"in.ctx_len", "in.new_len", "in.pages_held", "in.free_pages", "in.free_count"};
+  const void* outs[] = {out->row_start, out->kv_len, out->seq, out->pos, out->slot, out->pages_held, out->free_count,
+                        out->missing};
+  const char* out_names[] = {"out.row_start", "out.kv_len", "out.seq", "out.pos", "out.slot", "out.pages_held",
+                             "out.free_count", "out.missing"};
+  if (in->free_capacity < 0) return fail(SAS_ERR_INVALID_ARGUMENT, "free_capacity is negative");
+  for (int i = 0; i < 5; ++i) SAS_TRY(check_ptr(ins[i], in_names[i], i != 3 || in->free_capacity > 0));
+  for (int j = 0; j < 8; ++j) {
+    SAS_TRY(check_ptr(outs[j], out_names[j], true));
+    for (int i = 0; i < 5; ++i)
+      if (outs[j] == ins[i]) return fail(SAS_ERR_INVALID_ARGUMENT, "%s is %s", out_names[j], in_names[i]);
+  }
+  SAS_TRY(check_ptr(cache->block_table, "cache.block_table", true));
+  const int ps = cache->page_size;
+  if (ps <= 0 || cache->num_pages <= 0 || cache->max_pages_per_seq <= 0)
+    return fail(SAS_ERR_INVALID_ARGUMENT, "cache geometry must be positive (page_size %d, num_pages %d, "
+                "max_pages_per_seq %d)", ps, cache->num_pages, cache->max_pages_per_seq);
+  if (ps > 128 || (ps & (ps - 1)))
+    return fail(SAS_ERR_UNSUPPORTED, "page_size %d (supported: powers of two up to 128)", ps);
+  PlanArgs a = {};
+  a.b = batch;
+  a.rows = rows;
+  a.ps_shift = shift_of(ps);
+  a.num_pages = cache->num_pages;
+  a.max_pages = cache->max_pages_per_seq;
+  a.free_capacity = in->free_capacity;
+  a.ctx_len = in->ctx_len;
+  a.new_len = in->new_len;
+  a.held = in->pages_held;
+  a.free_pages = in->free_pages;
+  a.free_count = in->free_count;
+  a.table = (int32_t*)cache->block_table;
+  a.row_start = out->row_start;
+  a.kv_len = out->kv_len;
+  a.seq = out->seq;
+  a.pos = out->pos;
+  a.slot = out->slot;
+  a.held_out = out->pages_held;
+  a.free_out = out->free_count;
+  a.missing = out->missing;
+  hipStream_t s = (hipStream_t)stream;
+  Timed tm("plan_chunk", s);
+  HIP_TRY(launch_plan_chunk(a, s), "chunk plan");
+  return SAS_OK;
+}
+
+sas_status sas_qk_norm_rope(const sas_config* c, int32_t rows, const sas_rotary* rot, const sas_qkv* in, void* q_out,
+                            void* k_out, void* stream) {
+  QkArgs a;
+  SAS_TRY(qk_args(c, rows, rot, in, false, a));
+  SAS_TRY(check_ptr(q_out, "q_out", true));
+  SAS_TRY(check_ptr(k_out, "k_out", true));
+  SAS_TRY(check_in_place(in->q, a.qs, a.H, a.dh, q_out, "q_out"));
+  SAS_TRY(check_in_place(in->k, a.ks, a.Hkv, a.dh, k_out, "k_out"));
+  a.q_out = q_out;
+  a.k_out = k_out;
+  hipStream_t s = (hipStream_t)stream;
+  Timed tm("qk_norm_rope", s);
+  HIP_TRY(launch_qk_norm_rope(c->dtype, a, s), "q/k norm and rotation");
+  return SAS_OK;
+}
+
+sas_status sas_qk_norm_rope_backward(const sas_config* c, int32_t rows, const sas_rotary* rot, const sas_qkv* in,
+                                     const void* d_q_out, const void* d_k_out, void* dq, void* dk, float* dgain_q,
+                                     float* dgain_k, void* ws, size_t ws_bytes, void* stream) {
+  QkArgs a;
+  SAS_TRY(qk_args(c, rows, rot, in, false, a));
+  SAS_TRY(check_ptr(d_q_out, "d_q_out", true));
+  SAS_TRY(check_ptr(d_k_out, "d_k_out", true));
+  SAS_TRY(check_ptr(dq, "dq", true));
+  SAS_TRY(check_ptr(dk, "dk", true));
+  SAS_TRY(check_ptr(dgain_q, "dgain_q", rot->gain_q != nullptr));
+  SAS_TRY(check_ptr(dgain_k, "dgain_k", rot->gain_k != nullptr));
+  if ((dgain_q && !rot->gain_q) || (dgain_k && !rot->gain_k))
+    return fail(SAS_ERR_INVALID_ARGUMENT, "a gain's gradient without the gain");
+  for (const void* o : {dq, dk})
+    for (const void* i : {in->q, in->k, d_q_out, d_k_out})
+      if (o == i) return fail(SAS_ERR_INVALID_ARGUMENT, "dq or dk is an input");
+  Carve cv(ws);
+  float* part = carve_qk_backward(cv, c);
+  SAS_TRY(check_ws(ws, ws_bytes, cv.off));
+  a.dq_out = d_q_out;
+  a.dk_out = d_k_out;
+  a.dq = dq;
+  a.dk = dk;
+  a.dgain_q = dgain_q;
+  a.dgain_k = dgain_k;
+  a.part = dgain_q || dgain_k ? part : nullptr;
+  hipStream_t s = (hipStream_t)stream;
+  Timed tm("qk_norm_rope_bwd", s);
+  HIP_TRY(launch_qk_norm_rope_backward(c->dtype, a, s), "q/k norm and rotation backward");
+  return SAS_OK;
+}
+
+sas_status sas_cache_append(const sas_config* c, int32_t batch, int32_t rows, const sas_rotary* rot,
+                            const sas_qkv* in, const int64_t* slot, const int32_t* ctx_len, const int32_t* kv_len,
+                            const void* w_gk, const sas_paged_kv* cache, void* q_out, void* stream) {
+  SAS_TRY(check_chunk(batch, rows));
+  QkArgs a;
+  SAS_TRY(qk_args(c, rows, rot, in, true, a));
+  SAS_TRY(check_ptr(slot, "slot", true));
+  SAS_TRY(check_ptr(ctx_len, "ctx_len", true));
+  SAS_TRY(check_ptr(kv_len, "kv_len", true));
+  SAS_TRY(check_ptr(w_gk, "w_gk", false));
+  SAS_TRY(check_ptr(q_out, "q_out", true));
+  SAS_TRY(check_in_place(in->q, a.qs, a.H, a.dh, q_out, "q_out"));
+  if (!cache) return fail(SAS_ERR_INVALID_ARGUMENT, "cache is NULL");
+  SAS_TRY(check_cache(c, cache));
+  a.q_out = q_out;
+  a.slot = slot;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.num_pages = cache->num_pages;
+  a.ps_shift = shift_of(cache->page_size);
+  BlockSumArgs b = {};
+  b.b = batch;
+  b.rows = rows;
+  b.Hkv = a.Hkv;
+  b.dh = a.dh;
+  b.B = c->block_size;
+  b.ps_shift = a.ps_shift;
+  b.num_pages = cache->num_pages;
+  b.max_pages = cache->max_pages_per_seq;
+  b.max_blocks = cache->max_blocks;
+  b.ctx_len = ctx_len;
+  b.kv_len = kv_len;
+  b.table = cache->block_table;
+  b.k_pages = cache->k_pages;
+  b.w_gk = w_gk;
+  b.k_summary = cache->k_summary;
+  hipStream_t s = (hipStream_t)stream;
+  {
+    Timed tm("chunk_append", s);
+    HIP_TRY(launch_qk_norm_rope(c->dtype, a, s), "chunk append");
+  }
+  Timed tm("chunk_summaries", s);
+  HIP_TRY(launch_chunk_summaries(c->dtype, b, s), "chunk summaries");
+  return SAS_OK;
+}
+
+sas_status sas_attention_chunk(const sas_config* c, int32_t batch, int32_t rows, const void* q,
+                               const int32_t* row_start, const int32_t* kv_len, const sas_paged_kv* cache, void* o,
+                               float* lse, void* ws, size_t ws_bytes, void* stream) {
+  SAS_TRY(check_config(c, false));
+  SAS_TRY(check_chunk(batch, rows));
+  SAS_TRY(check_ptr(q, "q", true));
+  SAS_TRY(check_ptr(row_start, "row_start", true));
+  SAS_TRY(check_ptr(kv_len, "kv_len", true));
+  SAS_TRY(check_ptr(o, "o", true));
+  SAS_TRY(check_ptr(lse, "lse", false));
+  if (!cache) return fail(SAS_ERR_INVALID_ARGUMENT, "cache is NULL");
+  SAS_TRY(check_cache(c, cache));
+  if (c->n_heads / c->n_kv_heads > 128)
+    return fail(SAS_ERR_UNSUPPORTED, "%d query heads per KV head (supported: <= 128)", c->n_heads / c->n_kv_heads);
+  if ((long long)cache->max_pages_per_seq * cache->page_size > CHUNK_MAX_KEYS)
+    return fail(SAS_ERR_UNSUPPORTED, "the block table covers %lld positions (supported: <= 2^30)",
+                (long long)cache->max_pages_per_seq * cache->page_size);
+  if ((long long)rows * c->n_heads > INT32_MAX / 2)
+    return fail(SAS_ERR_UNSUPPORTED, "%d rows of %d heads (supported: <= 2^30 heads)", rows, c->n_heads);
+  Carve cv(ws);
+  const ChunkWs w = carve_chunk(cv, ws_bytes, c, batch);
+  SAS_TRY(check_ws(ws, ws_bytes, w.need));
+  ChunkArgs a = {};
+  a.b = batch;
+  a.rows = rows;
+  a.H = c->n_heads;
+  a.Hkv = c->n_kv_heads;
+  a.dh = c->head_dim;
+  a.sm_scale = sm_scale_of(c);
+  a.Q = q;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.table = cache->block_table;
+  a.num_pages = cache->num_pages;
+  a.ps_shift = shift_of(cache->page_size);
+  a.max_pages = cache->max_pages_per_seq;
+  a.row_start = row_start;
+  a.kv_len = kv_len;
+  a.O = o;
+  a.lse = lse;
+  a.head = w.head;
+  a.job_base = w.job_base;
+  a.seq_parts = w.seq_parts;
+  a.part_slots = w.part_slots;
+  a.part_o = w.part;
+  a.part_ml = w.part ? w.part + (size_t)w.part_slots * 128 * c->head_dim : nullptr;
+  hipStream_t s = (hipStream_t)stream;
+  Timed tm("attention_chunk", s);
+  HIP_TRY(launch_chunk_attention(c->dtype, a, s), "chunk attention");
+  return SAS_OK;
+}
+
+sas_status sas_verify_drafts(int32_t batch, int32_t rows, int32_t vocab, int32_t max_draft, const sas_verify_in* in,
+                             int32_t* out_tokens, int32_t* accepted, void* ws, size_t ws_bytes, void* stream) {
+  if (batch <= 0 || rows < 0 || vocab <= 0 || max_draft < 0)
+    return fail(SAS_ERR_INVALID_ARGUMENT, "batch %d and vocab %d must be positive, rows %d and max_draft %d >= 0",
+                batch, vocab, rows, max_draft);
+  if (batch > CHUNK_MAX_SEQS)
+    return fail(SAS_ERR_UNSUPPORTED, "batch %d (supported: <= %d sequences)", batch, CHUNK_MAX_SEQS);
+  if (vocab > (1 << 30) || max_draft > (1 << 30))
+    return fail(SAS_ERR_UNSUPPORTED, "vocab %d or max_draft %d (supported: <= 2^30)", vocab, max_draft);
+  if (rows > INT32_MAX - CHUNK_MAX_SEQS) return fail(SAS_ERR_UNSUPPORTED, "rows %d", rows);
+  if (!in) return fail(SAS_ERR_INVALID_ARGUMENT, "in is NULL");
+  SAS_TRY(check_ptr(in->target, "in.target", true));
+  SAS_TRY(check_ptr(in->draft, "in.draft", false));
+  SAS_TRY(check_ptr(in->tokens, "in.tokens", rows > 0));
+  SAS_TRY(check_ptr(in->draft_start, "in.draft_start", true));
+  SAS_TRY(check_ptr(in->u_accept, "in.u_accept", rows > 0));
+  SAS_TRY(check_ptr(in->u_sample, "in.u_sample", true));
+  SAS_TRY(check_ptr(out_tokens, "out_tokens", true));
+  SAS_TRY(check_ptr(accepted, "accepted", true));
+  SAS_TRY(check_ws(ws, ws_bytes, verify_part_bytes(batch)));
+  VerifyArgs a = {};
+  a.b = batch;
+  a.vocab = vocab;
+  a.max_draft = max_draft;
+  a.rows = rows;
+  a.target = in->target;
+  a.draft = in->draft;
+  a.tokens = in->tokens;
+  a.start = in->draft_start;
+  a.u_accept = in->u_accept;
+  a.u_sample = in->u_sample;
+  a.out = out_tokens;
+  a.accepted = accepted;
+  a.part = (double*)ws;
+  hipStream_t s = (hipStream_t)stream;
+  Timed tm("verify_drafts", s);
+  HIP_TRY(launch_verify_drafts(a, s), "draft verification");
   return SAS_OK;
 }
 

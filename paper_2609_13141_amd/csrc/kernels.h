@@ -376,6 +376,91 @@ hipError_t launch_decode_select(int dtype, const void* q, const DecodeArgs& c, i
 hipError_t launch_decode_attention(int dtype, const void* q, const DecodeArgs& c, const int32_t* sel,
                                    float* part_ml, float* part_o, void* O, hipStream_t s);
 
+// ---- chunk_plan.hip --------------------------------------------------------
+// Sequences of one call (their prefix sums are held in LDS).
+constexpr int CHUNK_MAX_SEQS = 4096;
+struct PlanArgs {
+  int b, rows, ps_shift, num_pages, max_pages, free_capacity;
+  const int32_t *ctx_len, *new_len, *held, *free_pages, *free_count;
+  int32_t* table;         // [b, max_pages]
+  int32_t *row_start, *kv_len, *seq, *pos, *held_out, *free_out, *missing;
+  int64_t* slot;
+};
+hipError_t launch_plan_chunk(const PlanArgs& a, hipStream_t s);
+
+// ---- qk_norm.hip -----------------------------------------------------------
+// Per-head RMSNorm and rotation of the rows of q and k (see sas_qk_norm_rope),
+// optionally into the pages of the rows' slots (with v).
+struct QkArgs {
+  int rows, H, Hkv, dh, axes, sec0, sec1;  // pairs [0, sec0) turn by axis 0, [sec0, sec0 + sec1) by axis 1
+  float eps;
+  double log2_base;
+  const void *q, *k, *v;
+  long long qs, ks, vs;    // elements between rows
+  const void *gain_q, *gain_k;
+  const int32_t* pos;      // [axes, rows]
+  void *q_out, *k_out;     // [rows, H, dh], [rows, Hkv, dh] or null
+  // cache (slot != null): K and V rows go to slot[r] = page * page_size + offset
+  const int64_t* slot;
+  void *k_pages, *v_pages;
+  int num_pages, ps_shift;
+  // backward: gradients of the outputs in, of q and k out; dgain [2, dh] fp32 (q, k) or null
+  const void *dq_out, *dk_out;
+  void *dq, *dk;
+  float *dgain_q, *dgain_k, *part;  // part [QK_BWD_GROUPS, 2, dh]
+};
+constexpr int QK_BWD_GROUPS = 1024;  // workgroups of the backward (partial sums of the gains' gradients)
+hipError_t launch_qk_norm_rope(int dtype, const QkArgs& a, hipStream_t s);
+hipError_t launch_qk_norm_rope_backward(int dtype, const QkArgs& a, hipStream_t s);
+// Summaries of the blocks that positions ctx_len[i] .. kv_len[i] - 1 complete, from
+// the pages; `rows` bounds the new positions of all sequences.
+struct BlockSumArgs {
+  int b, rows, Hkv, dh, B, ps_shift, num_pages, max_pages, max_blocks;
+  const int32_t *ctx_len, *kv_len, *table;
+  const void *k_pages, *w_gk;
+  void* k_summary;
+};
+hipError_t launch_chunk_summaries(int dtype, const BlockSumArgs& a, hipStream_t s);
+
+// ---- chunk_attention.hip ---------------------------------------------------
+struct ChunkArgs {
+  int b, rows, H, Hkv, dh;
+  float sm_scale;
+  const void* Q;           // [rows, H, dh]
+  const void *k_pages, *v_pages;
+  const int32_t* table;    // [b, max_pages]
+  int num_pages, ps_shift, max_pages;
+  const int32_t* row_start;  // [b + 1]
+  const int32_t* kv_len;     // [b]
+  void* O;                 // [rows, H, dh]
+  float* lse;              // [rows, H] or null
+  // scratch: the division of the work, written by the launch's first kernel
+  int32_t* head;           // [16]
+  int32_t* job_base;       // [b] first job of each sequence
+  int2* seq_parts;         // [b] parts of its tiles, first slot
+  float* part_o;           // [part_slots, 128, dh]
+  float* part_ml;          // [part_slots, 128, 2]
+  long long part_slots;    // 0: no tile is divided
+};
+// Parts that a call works best with: twice the workgroups that the chip holds, which is
+// the most that parts of the average work of a workgroup can come to.
+constexpr long long CHUNK_PART_SLOTS = 1024;
+constexpr int CHUNK_MIN_TILES = 2;  // key tiles of the least part
+constexpr long long CHUNK_MAX_KEYS = 1ll << 30;  // positions that a block table may cover
+hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s);
+
+// ---- verify.hip ------------------------------------------------------------
+struct VerifyArgs {
+  int b, vocab, max_draft, rows;   // rows: drafted tokens of all sequences
+  const float *target, *draft;     // [rows + b, vocab], [rows, vocab] or null
+  const int32_t *tokens, *start;   // [rows], [b + 1]
+  const float *u_accept, *u_sample;
+  int32_t *out, *accepted;         // [b, max_draft + 1], [b]
+  double* part;                    // [b, VERIFY_PIECES, 2] sums of the pieces of the weights
+};
+constexpr int VERIFY_PIECES = 32;
+hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s);
+
 // ---- model_ends.hip --------------------------------------------------------
 hipError_t launch_embed(int dtype, int b, int n, const int32_t* ids, const void* table, int vocab,
                         const void* img, int n_img, void* x, int d, hipStream_t s);

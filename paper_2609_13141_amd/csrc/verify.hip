@@ -1,0 +1,189 @@
+// Verification of drafted tokens against the target's probabilities.
+//
+// Sequence i drafted m tokens x_0 .. x_{m-1}; they are accepted in order while
+// u_j q_j(x_j) < p_j(x_j).  One more token is drawn by the inverse CDF of the
+// sequence's uniform u: from max(p - q, 0) at the first token that was not
+// accepted (from p without x_j when the draft has no probabilities; from p
+// itself when nothing is left), from p after the last when all were.
+//
+// Only one row of p and one of q are read in full, b vocab (4 or 8) bytes:
+// verify_sum_kernel cuts them into VERIFY_PIECES pieces, a workgroup each, and
+// leaves the pieces' sums; verify_pick_kernel finds the piece that the uniform
+// falls into and rescans that piece alone.  Differences and sums are fp64: the
+// fp32 inputs' products and differences are exact there, and a token's border
+// in the CDF is some 1e-16 wide rather than the 1e-7 of an fp32 sum.
+#include "common.h"
+#include "kernels.h"
+
+namespace sas {
+
+constexpr int VERIFY_NT = 256;
+
+// The rows that sequence i's last token is drawn from, found by the first wave.
+struct VerifyRow {
+  int acc;          // accepted tokens
+  const float* p;   // target row
+  const float* q;   // draft row, or null
+  int skip;         // token that is left out (a draft without probabilities), or -1
+};
+__device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i) {
+  const int lane = threadIdx.x & 63;
+  const int r0 = min(max(P.start[i], 0), P.rows);
+  const int m = min(min(max(P.start[i + 1], r0), P.rows) - r0, P.max_draft);
+  // 64 drafted tokens at a time; the first that is not accepted ends the search
+  int acc = m;
+  for (int j0 = 0; j0 < m; j0 += 64) {
+    const int j = j0 + lane;
+    bool ok = true;
+    if (j < m) {
+      const int x = P.tokens[r0 + j];
+      ok = false;
+      if (x >= 0 && x < P.vocab) {
+        const double px = P.target[(size_t)(r0 + i + j) * P.vocab + x];
+        const double qx = P.draft ? P.draft[(size_t)(r0 + j) * P.vocab + x] : 1.0;
+        ok = (double)P.u_accept[r0 + j] * qx < px;
+      }
+    }
+    const unsigned long long no = __builtin_amdgcn_ballot_w64(!ok);
+    if (no) {
+      acc = j0 + __builtin_ctzll(no);
+      break;
+    }
+  }
+  VerifyRow v;
+  v.acc = acc;
+  v.p = P.target + (size_t)(r0 + i + acc) * P.vocab;
+  const bool stop = acc < m;
+  v.q = stop && P.draft ? P.draft + (size_t)(r0 + acc) * P.vocab : nullptr;
+  v.skip = stop && !P.draft ? P.tokens[r0 + acc] : -1;
+  return v;
+}
+
+// weights of token e: (left over, target); negative and NaN values count as zero
+__device__ __forceinline__ double verify_pos(double x) { return x > 0.0 ? x : 0.0; }
+__device__ __forceinline__ double verify_left(const VerifyRow& v, int e, float p, float q) {
+  return e == v.skip ? 0.0 : verify_pos((double)p - (double)q);
+}
+
+__device__ __forceinline__ double wave_sum_f64(double x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+
+__global__ void __launch_bounds__(VERIFY_NT) verify_sum_kernel(VerifyArgs P, int len) {
+  __shared__ double red[2][VERIFY_NT / 64];
+  const int i = blockIdx.y, piece = blockIdx.x;
+  const VerifyRow v = verify_row(P, i);
+  const int e0 = piece * len, e1 = min(e0 + len, P.vocab);
+  double left = 0.0, all = 0.0;
+  for (int e = e0 + threadIdx.x; e < e1; e += VERIFY_NT) {
+    const float p = v.p[e], q = v.q ? v.q[e] : 0.f;
+    left += verify_left(v, e, p, q);
+    all += verify_pos((double)p);
+  }
+  left = wave_sum_f64(left);
+  all = wave_sum_f64(all);
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x >> 6] = left;
+    red[1][threadIdx.x >> 6] = all;
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    double t = 0.0;
+    for (int w = 0; w < VERIFY_NT / 64; ++w) t += red[threadIdx.x][w];
+    P.part[((size_t)i * gridDim.x + piece) * 2 + threadIdx.x] = t;
+  }
+}
+
+__global__ void __launch_bounds__(VERIFY_NT) verify_pick_kernel(VerifyArgs P, int len, int pieces) {
+  __shared__ double wsum[VERIFY_NT / 64];
+  __shared__ int found[2];  // the first token past the uniform, the last of any weight
+  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  VerifyRow v = verify_row(P, i);
+  const double* part = P.part + (size_t)i * pieces * 2;
+  double tot[2] = {0.0, 0.0};
+  for (int k = 0; k < pieces; ++k) {
+    tot[0] += part[2 * k];
+    tot[1] += part[2 * k + 1];
+  }
+  const int which = tot[0] > 0.0 ? 0 : 1;  // nothing left over: the target itself
+  if (which == 1) {
+    v.q = nullptr;
+    v.skip = -1;
+  }
+  const double aim = (double)P.u_sample[i] * tot[which];
+  // the first piece whose end lies past the aim (the last of any weight when none does)
+  int piece = -1, last = -1;
+  double before = 0.0, run = 0.0, lastb = 0.0;
+  for (int k = 0; k < pieces && piece < 0; ++k) {
+    const double w = part[2 * k + which];
+    if (w > 0.0) {
+      last = k;
+      lastb = run;
+    }
+    if (run + w > aim) {
+      piece = k;
+      before = run;
+    }
+    run += w;
+  }
+  if (piece < 0) {
+    piece = last;
+    before = lastb;
+  }
+  if (tid == 0) {
+    found[0] = 0x7fffffff;
+    found[1] = -1;
+  }
+  __syncthreads();
+  if (piece >= 0) {
+    const int e0 = piece * len, e1 = min(e0 + len, P.vocab);
+    // 256 tokens at a time, in order
+    for (int b0 = e0; b0 < e1; b0 += VERIFY_NT) {
+      const int e = b0 + tid;
+      const double w = e < e1 ? verify_left(v, e, v.p[e], v.q ? v.q[e] : 0.f) : 0.0;
+      double x = w;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+      }
+      if (lane == 63) wsum[wave] = x;
+      __syncthreads();
+      double at = before, sum = 0.0;
+      for (int k = 0; k < VERIFY_NT / 64; ++k) {
+        if (k < wave) at += wsum[k];
+        sum += wsum[k];
+      }
+      if (w > 0.0) {
+        if (at + x > aim) atomicMin(&found[0], e);
+        atomicMax(&found[1], e);
+      }
+      before += sum;
+      __syncthreads();
+      if (found[0] != 0x7fffffff) break;
+    }
+  }
+  __syncthreads();
+  const int W = P.max_draft + 1;
+  const int r0 = min(max(P.start[i], 0), P.rows);
+  for (int j = tid; j < W; j += VERIFY_NT) {
+    int t = -1;
+    if (j < v.acc) t = P.tokens[r0 + j];
+    else if (j == v.acc) t = found[0] != 0x7fffffff ? found[0] : found[1];
+    P.out[(size_t)i * W + j] = t;
+  }
+  if (tid == 0) P.accepted[i] = v.acc;
+}
+
+hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s) {
+  // pieces of whole 256-token steps
+  const int steps = cdiv(a.vocab, VERIFY_NT), pieces = std::min(VERIFY_PIECES, steps);
+  const int len = cdiv(steps, pieces) * VERIFY_NT;
+  verify_sum_kernel<<<dim3(pieces, a.b), VERIFY_NT, 0, s>>>(a, len);
+  verify_pick_kernel<<<a.b, VERIFY_NT, 0, s>>>(a, len, pieces);
+  return hipGetLastError();
+}
+
+}  // namespace sas

@@ -24,13 +24,14 @@ GATE_POS = {"inner": 0, "outer": 1}
 GATE_ACT = {"softmax": 0, "sigmoid": 1, "raw": 2}
 SCOPES = {"sparse": 0, "full": 1}
 (OP_ATTENTION, OP_MLP, OP_LAYER, OP_DECODE, OP_LM_HEAD, OP_DECODE_SELECT, OP_ATTENTION_BACKWARD,
- OP_SELECTOR_BACKWARD, OP_SELECTION_STATS) = range(9)
+ OP_SELECTOR_BACKWARD, OP_SELECTION_STATS, OP_QK_BACKWARD, OP_ATTENTION_CHUNK, OP_VERIFY_DRAFTS) = range(12)
 TORCH_DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 EXPORTS = ("sas_workspace_size", "sas_attention_prefill", "sas_mlp_forward", "sas_layer_forward",
            "sas_decode_step", "sas_decode_step_noalloc", "sas_decode_select", "sas_attention_backward", "sas_selector_backward", "sas_selection_stats", "sas_overlap_recall", "sas_embed", "sas_lm_head_argmax", "sas_last_error", "sas_version",
            "sas_profiler_start", "sas_profiler_select", "sas_profiler_stop", "sas_profiler_record",
-           "sas_decode_packed_bytes", "sas_pack_decode_weights")
+           "sas_decode_packed_bytes", "sas_pack_decode_weights", "sas_plan_chunk", "sas_qk_norm_rope",
+           "sas_qk_norm_rope_backward", "sas_cache_append", "sas_attention_chunk", "sas_verify_drafts")
 
 
 class SasError(RuntimeError):
@@ -97,6 +98,30 @@ class PagedKV(C.Structure):
                 ("max_pages_per_seq", C.c_int32), ("max_blocks", C.c_int32)]
 
 
+class PlanIn(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("ctx_len", "new_len", "pages_held", "free_pages", "free_count")] + \
+               [("free_capacity", C.c_int32)]
+
+
+class PlanOut(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("row_start", "kv_len", "seq", "pos", "slot", "pages_held", "free_count",
+                                          "missing")]
+
+
+class Rotary(C.Structure):
+    _fields_ = [("gain_q", C.c_void_p), ("gain_k", C.c_void_p), ("pos", C.c_void_p), ("axes", C.c_int32),
+                ("section", C.c_int32 * 3)]
+
+
+class Qkv(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
+class VerifyIn(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("target", "draft", "tokens", "draft_start", "u_accept", "u_sample")]
+
+
 _lib = None
 
 
@@ -158,6 +183,20 @@ def lib() -> C.CDLL:
     L.sas_profiler_stop.argtypes = []
     L.sas_profiler_record.restype = i32
     L.sas_profiler_record.argtypes = [i32, C.POINTER(C.c_char_p), C.POINTER(C.c_float)]
+    L.sas_plan_chunk.restype = i32
+    L.sas_plan_chunk.argtypes = [i32, i32, C.POINTER(PlanIn), C.POINTER(PagedKV), C.POINTER(PlanOut), vp]
+    L.sas_qk_norm_rope.restype = i32
+    L.sas_qk_norm_rope.argtypes = [C.POINTER(Config), i32, C.POINTER(Rotary), C.POINTER(Qkv), vp, vp, vp]
+    L.sas_qk_norm_rope_backward.restype = i32
+    L.sas_qk_norm_rope_backward.argtypes = [C.POINTER(Config), i32, C.POINTER(Rotary), C.POINTER(Qkv), vp, vp, vp, vp,
+                                            vp, vp, vp, sz, vp]
+    L.sas_cache_append.restype = i32
+    L.sas_cache_append.argtypes = [C.POINTER(Config), i32, i32, C.POINTER(Rotary), C.POINTER(Qkv), vp, vp, vp, vp,
+                                   C.POINTER(PagedKV), vp, vp]
+    L.sas_attention_chunk.restype = i32
+    L.sas_attention_chunk.argtypes = [C.POINTER(Config), i32, i32, vp, vp, vp, C.POINTER(PagedKV), vp, vp, vp, sz, vp]
+    L.sas_verify_drafts.restype = i32
+    L.sas_verify_drafts.argtypes = [i32, i32, i32, i32, C.POINTER(VerifyIn), vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -529,6 +568,220 @@ def lm_head_argmax(cfg: Config, h, gamma, w_lm, *, logits: bool = False, ws: Wor
     _check(lib().sas_lm_head_argmax(C.byref(cfg), b, _ptr(h), _ptr(gamma), _ptr(w_lm), V, _ptr(lg), _ptr(tok),
                                     wsp, wsn, _stream()))
     return tok, lg
+
+
+# ---- chunks of new tokens over the paged cache ----------------------------------
+# These calls run on the device of their tensors and its current stream.  Without
+# `ws` each takes its scratch from torch's allocator, so that calls on several
+# streams, and captured ones, share none; a given Workspace is for one stream.
+
+def _need(name: str, t, dtype, shape, dev):
+    """t is a contiguous tensor of that type and shape on `dev` (-1: any size)."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev or t.dim() != len(shape) \
+            or any(w not in (-1, n) for n, w in zip(t.shape, shape)) or not t.is_contiguous():
+        got = f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}" if isinstance(t, torch.Tensor) \
+            else type(t).__name__
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name}: expected contiguous {dtype} {list(shape)} on {dev}, got {got}")
+
+
+def _device(name: str, t):
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name} is not a tensor on the GPU")
+    return t.device
+
+
+def _act(cfg: Config):
+    return torch.bfloat16 if cfg.dtype == SAS_BF16 else torch.float32
+
+
+def _scratch(ws: Workspace | None, nbytes: int, dev):
+    """(buffer to keep until the call has returned, its pointer, its size)."""
+    if nbytes == 0:
+        return None, None, 0
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=dev) if ws is None else ws.get(nbytes)[0]
+    return buf, _ptr(buf), buf.numel()
+
+
+def _need_cache(cfg: Config, cache: PagedCache, b: int, dev):
+    Hkv, dh = cfg.n_kv_heads, cfg.head_dim
+    _need("cache.k_pages", cache.k_pages, _act(cfg), (-1, Hkv, cache.page_size, dh), dev)
+    _need("cache.v_pages", cache.v_pages, _act(cfg), tuple(cache.k_pages.shape), dev)
+    _need("cache.block_table", cache.block_table, torch.int32, (b, -1), dev)
+    _need("cache.k_summary", cache.k_summary, _act(cfg), (b, Hkv, -1, dh), dev)
+
+
+def _rows_of(cfg: Config, name: str, t, heads: int, rows: int, dev):
+    """Elements between the rows of head rows [rows, heads, dh], whose rows are contiguous."""
+    dh = cfg.head_dim
+    if not isinstance(t, torch.Tensor) or t.dtype != _act(cfg) or t.device != dev or tuple(t.shape) != (rows, heads, dh) \
+            or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh):
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name}: expected {_act(cfg)} [{rows}, {heads}, {dh}] on {dev} with "
+                       "contiguous rows")
+    return t.stride(0) if rows > 1 else heads * dh
+
+
+def _rotary(cfg: Config, pos, gain_q, gain_k, sections, rows: int, dev) -> Rotary:
+    sections = (cfg.head_dim // 2,) if sections is None else tuple(int(n) for n in sections)
+    if not 1 <= len(sections) <= 3:
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"sections {sections}: 1 to 3 axes")
+    if isinstance(pos, torch.Tensor) and pos.dim() == 1:
+        pos = pos[None]
+    _need("pos", pos, torch.int32, (len(sections), rows), dev)
+    for name, g in (("gain_q", gain_q), ("gain_k", gain_k)):
+        if g is not None:
+            _need(name, g, _act(cfg), (cfg.head_dim,), dev)
+    return Rotary(_ptr(gain_q), _ptr(gain_k), _ptr(pos), len(sections), (C.c_int32 * 3)(*sections))
+
+
+def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free_count, rows: int) -> dict:
+    """Pages and slots of a chunk: ctx_len, new_len, pages_held [b], the stack
+    free_pages [capacity] with free_count [1] entries (all int32); `rows` rows
+    (at least the sum of new_len, or tokens go without).  Writes the new entries
+    of cache.block_table and returns row_start [b+1], kv_len [b], seq and pos
+    [rows], slot [rows] (int64), pages_held [b], free_count [1], missing [1]."""
+    dev = _device("ctx_len", ctx_len)
+    b = ctx_len.numel()
+    i32 = torch.int32
+    for name, t in (("ctx_len", ctx_len), ("new_len", new_len), ("pages_held", pages_held)):
+        _need(name, t, i32, (b,), dev)
+    _need("free_pages", free_pages, i32, (-1,), dev)
+    _need("free_count", free_count, i32, (1,), dev)
+    _need("cache.block_table", cache.block_table, i32, (b, -1), dev)
+    out = {"row_start": torch.empty(b + 1, dtype=i32, device=dev), "kv_len": torch.empty(b, dtype=i32, device=dev),
+           "seq": torch.empty(rows, dtype=i32, device=dev), "pos": torch.empty(rows, dtype=i32, device=dev),
+           "slot": torch.empty(rows, dtype=torch.int64, device=dev),
+           "pages_held": torch.empty(b, dtype=i32, device=dev), "free_count": torch.empty(1, dtype=i32, device=dev),
+           "missing": torch.empty(1, dtype=i32, device=dev)}
+    pi = PlanIn(_ptr(ctx_len), _ptr(new_len), _ptr(pages_held), _ptr(free_pages), _ptr(free_count),
+                free_pages.numel())
+    po = PlanOut(*[_ptr(out[f]) for f, _ in PlanOut._fields_])
+    with torch.cuda.device(dev):
+        _check(lib().sas_plan_chunk(b, rows, C.byref(pi), C.byref(cache.struct()), C.byref(po), _stream()))
+    return out
+
+
+def qk_norm_rope(cfg: Config, q, k, pos, gain_q=None, gain_k=None, *, sections=None):
+    """Normed and rotated heads (q', k') of q [rows, H, dh] and k [rows, Hkv, dh]
+    (views of a packed projection will do): RMSNorm over each head with gain_q /
+    gain_k [dh] (None: no norm), then the rotation by pos [axes, rows] int32 (or
+    [rows]), sections[a] rotary pairs turning by axis a (None: all by one)."""
+    dev = _device("q", q)
+    rows = q.shape[0]
+    qs, ks = _rows_of(cfg, "q", q, cfg.n_heads, rows, dev), _rows_of(cfg, "k", k, cfg.n_kv_heads, rows, dev)
+    rot = _rotary(cfg, pos, gain_q, gain_k, sections, rows, dev)
+    qo = torch.empty(rows, cfg.n_heads, cfg.head_dim, dtype=q.dtype, device=dev)
+    ko = torch.empty(rows, cfg.n_kv_heads, cfg.head_dim, dtype=q.dtype, device=dev)
+    if rows:
+        with torch.cuda.device(dev):
+            _check(lib().sas_qk_norm_rope(C.byref(cfg), rows, C.byref(rot), C.byref(Qkv(_ptr(q), _ptr(k), None, qs, ks, 0)),
+                                          _ptr(qo), _ptr(ko), _stream()))
+    return qo, ko
+
+
+def qk_norm_rope_backward(cfg: Config, q, k, pos, d_q, d_k, gain_q=None, gain_k=None, *, sections=None,
+                          ws: Workspace | None = None) -> dict:
+    """Gradients of qk_norm_rope's inputs from those of its outputs d_q, d_k:
+    dq, dk and, for given gains, dgain_q / dgain_k [dh] fp32."""
+    dev = _device("q", q)
+    rows = q.shape[0]
+    qs, ks = _rows_of(cfg, "q", q, cfg.n_heads, rows, dev), _rows_of(cfg, "k", k, cfg.n_kv_heads, rows, dev)
+    rot = _rotary(cfg, pos, gain_q, gain_k, sections, rows, dev)
+    _need("d_q", d_q, q.dtype, (rows, cfg.n_heads, cfg.head_dim), dev)
+    _need("d_k", d_k, q.dtype, (rows, cfg.n_kv_heads, cfg.head_dim), dev)
+    out = {"dq": torch.empty_like(d_q), "dk": torch.empty_like(d_k)}
+    new = torch.empty if rows else torch.zeros
+    for name, g in (("dgain_q", gain_q), ("dgain_k", gain_k)):
+        if g is not None:
+            out[name] = new(cfg.head_dim, dtype=torch.float32, device=dev)
+    if rows:
+        buf, wsp, wsn = _scratch(ws, workspace_size(cfg, OP_QK_BACKWARD, rows, 0), dev)
+        with torch.cuda.device(dev):
+            _check(lib().sas_qk_norm_rope_backward(
+                C.byref(cfg), rows, C.byref(rot), C.byref(Qkv(_ptr(q), _ptr(k), None, qs, ks, 0)), _ptr(d_q), _ptr(d_k),
+                _ptr(out["dq"]), _ptr(out["dk"]), _ptr(out.get("dgain_q")), _ptr(out.get("dgain_k")), wsp, wsn,
+                _stream()))
+    return out
+
+
+def cache_append(cfg: Config, cache: PagedCache, q, k, v, pos, slot, ctx_len, kv_len, gain_q=None, gain_k=None, *,
+                 sections=None, w_gk=None):
+    """A chunk's heads into the cache: q, k as qk_norm_rope's, v [rows, Hkv, dh];
+    slot [rows] int64, ctx_len and kv_len [b] int32 as plan_chunk's.  Writes the
+    keys, values and the summaries of the blocks that the chunk completes; returns
+    the normed and rotated queries."""
+    dev = _device("q", q)
+    rows, b = q.shape[0], ctx_len.numel()
+    H, Hkv = cfg.n_heads, cfg.n_kv_heads
+    qs, ks = _rows_of(cfg, "q", q, H, rows, dev), _rows_of(cfg, "k", k, Hkv, rows, dev)
+    vs = _rows_of(cfg, "v", v, Hkv, rows, dev)
+    rot = _rotary(cfg, pos, gain_q, gain_k, sections, rows, dev)
+    _need("slot", slot, torch.int64, (rows,), dev)
+    _need("ctx_len", ctx_len, torch.int32, (b,), dev)
+    _need("kv_len", kv_len, torch.int32, (b,), dev)
+    _need_cache(cfg, cache, b, dev)
+    if w_gk is not None:
+        _need("w_gk", w_gk, q.dtype, (Hkv, cfg.head_dim, cfg.head_dim), dev)
+    qo = torch.empty(rows, H, cfg.head_dim, dtype=q.dtype, device=dev)
+    if rows:
+        with torch.cuda.device(dev):
+            _check(lib().sas_cache_append(
+                C.byref(cfg), b, rows, C.byref(rot), C.byref(Qkv(_ptr(q), _ptr(k), _ptr(v), qs, ks, vs)), _ptr(slot),
+                _ptr(ctx_len), _ptr(kv_len), _ptr(w_gk), C.byref(cache.struct()), _ptr(qo), _stream()))
+    return qo
+
+
+def attention_chunk(cfg: Config, q, cache: PagedCache, row_start, kv_len, *, lse: bool = True, out=None,
+                    ws: Workspace | None = None) -> dict:
+    """Causal attention of a chunk's queries q [rows, H, dh] over the cache:
+    row_start [b+1] and kv_len [b] int32 as plan_chunk's, the chunk's keys in the
+    cache already.  o [rows, H, dh] (`out` when given; rows behind row_start[b] are
+    not written) and lse [rows, H] fp32."""
+    dev = _device("q", q)
+    rows, b = q.shape[0], kv_len.numel()
+    _need("q", q, _act(cfg), (rows, cfg.n_heads, cfg.head_dim), dev)
+    _need("row_start", row_start, torch.int32, (b + 1,), dev)
+    _need("kv_len", kv_len, torch.int32, (b,), dev)
+    _need_cache(cfg, cache, b, dev)
+    if out is not None:
+        _need("out", out, q.dtype, tuple(q.shape), dev)
+    r = {"o": torch.empty_like(q) if out is None else out}
+    if lse:
+        r["lse"] = torch.empty(rows, cfg.n_heads, dtype=torch.float32, device=dev)
+    if rows:
+        buf, wsp, wsn = _scratch(ws, workspace_size(cfg, OP_ATTENTION_CHUNK, b, rows), dev)
+        with torch.cuda.device(dev):
+            _check(lib().sas_attention_chunk(C.byref(cfg), b, rows, _ptr(q), _ptr(row_start), _ptr(kv_len),
+                                             C.byref(cache.struct()), _ptr(r["o"]), _ptr(r.get("lse")), wsp, wsn,
+                                             _stream()))
+    return r
+
+
+def verify_drafts(target, draft, tokens, draft_start, u_accept, u_sample, max_draft: int, *,
+                  ws: Workspace | None = None) -> dict:
+    """Speculative verification of drafted tokens [rows] int32, sequence i's at
+    draft_start[i] .. draft_start[i+1] - 1 (at most max_draft): target [rows + b, V]
+    and draft [rows, V] (or None) fp32 probabilities, u_accept [rows], u_sample [b]
+    fp32 uniforms.  tokens [b, max_draft + 1]: the accepted ones, the drawn one,
+    -1; accepted [b]."""
+    dev = _device("target", target)
+    rows, b = tokens.numel(), u_sample.numel()
+    f32, i32 = torch.float32, torch.int32
+    _need("target", target, f32, (rows + b, -1), dev)
+    V = target.shape[1]
+    if draft is not None:
+        _need("draft", draft, f32, (rows, V), dev)
+    _need("tokens", tokens, i32, (rows,), dev)
+    _need("draft_start", draft_start, i32, (b + 1,), dev)
+    _need("u_accept", u_accept, f32, (rows,), dev)
+    _need("u_sample", u_sample, f32, (b,), dev)
+    out = {"tokens": torch.empty(b, max(max_draft, 0) + 1, dtype=i32, device=dev),
+           "accepted": torch.empty(b, dtype=i32, device=dev)}
+    vi = VerifyIn(_ptr(target), _ptr(draft) if rows else None, *[_ptr(t) for t in (tokens, draft_start, u_accept, u_sample)])
+    buf, wsp, wsn = _scratch(ws, lib().sas_workspace_size(None, OP_VERIFY_DRAFTS, b, 0), dev)
+    with torch.cuda.device(dev):
+        _check(lib().sas_verify_drafts(b, rows, V, max_draft, C.byref(vi), _ptr(out["tokens"]), _ptr(out["accepted"]),
+                                       wsp, wsn, _stream()))
+    return out
 
 
 def to_device(arr, dtype: str, device="cuda"):
