@@ -736,17 +736,17 @@ struct ChunkWs {
   int2* seq_parts;
   size_t need;  // bytes up to here; the parts may be fewer
   float* part;
-  long long part_slots;
+  long long part_rows;
 };
-size_t chunk_part_bytes(const sas_config* c) { return (size_t)128 * (c->head_dim + 2) * 4; }
+size_t chunk_part_bytes(const sas_config* c) { return (size_t)(c->head_dim + 2) * 4; }
 ChunkWs carve_chunk(Carve& cv, size_t total, const sas_config* c, int b) {
   ChunkWs w;
   w.head = (int32_t*)cv.take(64);
   w.job_base = (int32_t*)cv.take((size_t)b * 4);
   w.seq_parts = (int2*)cv.take((size_t)b * 8);
   w.need = cv.off;
-  w.part_slots = CHUNK_PART_SLOTS;
-  w.part = (float*)cv.take_some(total, chunk_part_bytes(c), w.part_slots);
+  w.part_rows = CHUNK_PART_ROWS;
+  w.part = (float*)cv.take_some(total, chunk_part_bytes(c), w.part_rows);
   return w;
 }
 
@@ -1825,9 +1825,9 @@ sas_status sas_attention_chunk(const sas_config* c, int32_t batch, int32_t rows,
   a.head = w.head;
   a.job_base = w.job_base;
   a.seq_parts = w.seq_parts;
-  a.part_slots = w.part_slots;
+  a.part_rows = w.part_rows;
   a.part_o = w.part;
-  a.part_ml = w.part ? w.part + (size_t)w.part_slots * 128 * c->head_dim : nullptr;
+  a.part_ml = w.part ? w.part + (size_t)w.part_rows * c->head_dim : nullptr;
   hipStream_t s = (hipStream_t)stream;
   Timed tm("attention_chunk", s);
   HIP_TRY(launch_chunk_attention(c->dtype, a, s), "chunk attention");

@@ -7,11 +7,12 @@
 //
 // The lengths are device memory, so the work is divided on the device: a tile
 // is 128 rows (128 / G consecutive tokens x the G heads of a kv head, which
-// read the same keys), and chunk_plan_kernel cuts the tiles' key ranges into
-// parts of at most C key tiles, C the average work of a resident workgroup;
-// parts are merged by chunk_combine_kernel.  Workgroups take the jobs from
-// eight queues, one per XCD, each a contiguous share, so that the tiles of one
-// (sequence, kv head) read its keys from one L2.
+// read the same keys), and the tiles' key ranges are cut into parts of at most C
+// key tiles (chunk_part_length), merged by chunk_combine_kernel.  Jobs are
+// numbered so that those that read the same keys follow each other, and each XCD
+// takes a contiguous share, one job a workgroup where they all fit the chip at
+// once, through a queue per XCD otherwise.  Up to 64 sequences every workgroup
+// forms the division itself, a lane a sequence; more take a kernel of their own.
 //
 // The tile loop is that of the prefill kernel (S^T = K Q^T, P^T fed back from
 // registers as the B operand of O^T = V^T P^T) with rows found through the
@@ -21,6 +22,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "common.h"
 #include "kernels.h"
@@ -71,7 +73,55 @@ __device__ __forceinline__ int wave_find(const int* base, int n, int x, int lane
   return lo + 63 - __builtin_clzll(c);
 }
 
-// sum over the workgroup's 1024 threads of v, and the sum before this thread (s: 17 values of LDS)
+// The work of one sequence: (tile, kv head) pairs, key tiles of each (the last
+// tile's count: earlier ones have up to 128 / KEYS fewer), rows of a tile's part.
+struct ChunkWork {
+  int units, nk, prow;
+};
+__device__ __forceinline__ ChunkWork chunk_work(const ChunkArgs& P, const ChunkSeq& q, int keys_per_tile) {
+  const int G = P.H / P.Hkv, qpt = 128 / G;
+  ChunkWork w;
+  w.units = P.Hkv * ((q.m + qpt - 1) / qpt);
+  w.nk = (q.keys + keys_per_tile - 1) / keys_per_tile;
+  w.prow = min(q.m, qpt) * G;
+  return w;
+}
+__device__ __forceinline__ int chunk_parts(int nk, int C) { return max(1, (int)(((long long)nk + C - 1) / C)); }
+
+// The length C of a part, in key tiles.  With fewer (tile, head) pairs than resident
+// workgroups, the least C whose parts still fit them: one round of jobs, none longer
+// than it has to be.  With more, a part is the average work of a workgroup, which
+// only cuts tiles far longer than the others.  A divided tile has at most 2 nk / C
+// parts, so that C >= 2 sum(units nk prow) / part_rows keeps them inside the scratch.
+// sum(f): the sum over all sequences of f of their work, the same in every thread.
+template <typename Sum>
+__device__ __forceinline__ int chunk_part_length(const ChunkArgs& P, int res, Sum sum) {
+  if (P.part_rows <= 0) return 0x7fffffff;
+  const long long U = sum([](const ChunkWork& w) { return (long long)w.units; });
+  const long long W = sum([](const ChunkWork& w) { return (long long)w.units * w.nk; });
+  const long long R = sum([](const ChunkWork& w) { return (long long)w.units * w.nk * w.prow; });
+  const long long least = max((long long)CHUNK_MIN_TILES, (2 * R + P.part_rows - 1) / P.part_rows);
+  long long lo = max(least, (W + res - 1) / res);
+  if (U < res) {
+    // W / C + U parts at most: some C up to W / (res - U) fits
+    long long hi = max(lo, (W + res - U - 1) / (res - U));
+    while (lo < hi) {
+      const long long mid = (lo + hi) / 2;
+      const int C = (int)min(mid, 0x7fffffffll);
+      if (sum([C](const ChunkWork& w) { return (long long)w.units * chunk_parts(w.nk, C); }) <= res) hi = mid;
+      else lo = mid + 1;
+    }
+  }
+  return (int)min(lo, 0x7fffffffll);
+}
+
+__device__ __forceinline__ long long wave_sum_i64(long long v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// sum over the workgroup's 1024 threads of v, and the sum before this thread (s: 16 values of LDS)
 __device__ __forceinline__ long long scan1024(long long v, long long* s, long long& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   long long x = v;
@@ -93,57 +143,91 @@ __device__ __forceinline__ long long scan1024(long long v, long long* s, long lo
   return before + x - v;
 }
 
-// One workgroup: divides the work (see above) and clears the job queues.
-// head[0] = jobs, head[1] = C, head[8 + x] = the next job of XCD x's share.
-__global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_per_tile, int want_parts) {
-  __shared__ long long s[17];
+// One workgroup: divides the work of any number of sequences and clears the job queues.
+// head[0] = jobs, head[1] = whether a tile is divided, head[8 + x] = the next job of
+// XCD x's share.
+__global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_per_tile, int res) {
+  __shared__ long long s[16];
+  constexpr int MAX_PER = CHUNK_MAX_SEQS / 1024;
   const int tid = threadIdx.x, per = (P.b + 1023) / 1024;
-  const int qpt = 128 / (P.H / P.Hkv);
-  long long W = 0, total;
-  for (int u = 0; u < per; ++u) {
+  ChunkWork w[MAX_PER];
+#pragma unroll
+  for (int u = 0; u < MAX_PER; ++u) {
     const int i = tid * per + u;
-    if (i >= P.b) break;
-    const ChunkSeq q = chunk_seq(P, i);
-    W += (long long)P.Hkv * ((q.m + qpt - 1) / qpt) * ((q.keys + keys_per_tile - 1) / keys_per_tile);
+    w[u] = u < per && i < P.b ? chunk_work(P, chunk_seq(P, i), keys_per_tile) : ChunkWork{0, 0, 0};
   }
-  (void)scan1024(W, s, total);
-  // at most 2 W / C parts in all of the divided tiles: they fit the scratch
-  long long C = max((long long)CHUNK_MIN_TILES, (total + want_parts - 1) / want_parts);
-  C = P.part_slots > 0 ? max(C, (2 * total + P.part_slots - 1) / P.part_slots) : 0x7fffffffll;
-  long long jobs = 0, slots = 0;
-  for (int u = 0; u < per; ++u) {
-    const int i = tid * per + u;
-    if (i >= P.b) break;
-    const ChunkSeq q = chunk_seq(P, i);
-    const long long nk = (q.keys + keys_per_tile - 1) / keys_per_tile;
-    const long long parts = max(1ll, (nk + C - 1) / C);
-    const long long j = (long long)P.Hkv * ((q.m + qpt - 1) / qpt) * parts;
-    jobs += j;
-    if (parts > 1) slots += j;
+  const int C = chunk_part_length(P, res, [&](auto f) {
+    long long v = 0, total;
+#pragma unroll
+    for (int u = 0; u < MAX_PER; ++u) v += f(w[u]);
+    (void)scan1024(v, s, total);
+    return total;
+  });
+  long long jobs = 0, prows = 0;
+#pragma unroll
+  for (int u = 0; u < MAX_PER; ++u) {
+    const long long parts = chunk_parts(w[u].nk, C);
+    jobs += w[u].units * parts;
+    if (parts > 1) prows += w[u].units * parts * w[u].prow;
   }
-  long long njobs, nslots;
-  long long j0 = scan1024(jobs, s, njobs), s0 = scan1024(slots, s, nslots);
-  for (int u = 0; u < per; ++u) {
+  long long njobs, nrows;
+  long long j0 = scan1024(jobs, s, njobs), r0 = scan1024(prows, s, nrows);
+#pragma unroll
+  for (int u = 0; u < MAX_PER; ++u) {
     const int i = tid * per + u;
-    if (i >= P.b) break;
-    const ChunkSeq q = chunk_seq(P, i);
-    const long long nk = (q.keys + keys_per_tile - 1) / keys_per_tile;
-    const long long parts = max(1ll, (nk + C - 1) / C);
-    const long long j = (long long)P.Hkv * ((q.m + qpt - 1) / qpt) * parts;
+    if (u >= per || i >= P.b) continue;
+    const long long parts = chunk_parts(w[u].nk, C);
     P.job_base[i] = (int)j0;
-    P.seq_parts[i] = make_int2((int)parts, (int)s0);
-    j0 += j;
-    if (parts > 1) s0 += j;
+    P.seq_parts[i] = make_int2((int)parts, (int)r0);
+    j0 += w[u].units * parts;
+    if (parts > 1) r0 += w[u].units * parts * w[u].prow;
   }
   if (tid == 0) {
     P.head[0] = (int)njobs;
-    P.head[1] = nslots > 0;
+    P.head[1] = nrows > 0;
   }
   if (tid < ATTN_XCDS) P.head[8 + tid] = (int)(njobs * tid / ATTN_XCDS);
 }
 
+// The same division of at most 64 sequences by one wave, a lane a sequence: the job of
+// workgroup `block` (seq -1: none), its job within the sequence and its parts.
+struct ChunkJob {
+  int seq, rel;
+  int2 sp;
+};
+__device__ __forceinline__ ChunkJob chunk_wave_plan(const ChunkArgs& P, int keys_per_tile, int res, int block) {
+  const int lane = threadIdx.x & 63;
+  const ChunkWork w = lane < P.b ? chunk_work(P, chunk_seq(P, lane), keys_per_tile) : ChunkWork{0, 0, 0};
+  const int C = chunk_part_length(P, res, [&](auto f) { return wave_sum_i64(f(w)); });
+  const int parts = chunk_parts(w.nk, C);
+  const int jobs = w.units * parts, prows = parts > 1 ? jobs * w.prow : 0;
+  int j = jobs, r = prows;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int a = __shfl_up(j, o, 64), b = __shfl_up(r, o, 64);
+    if (lane >= o) {
+      j += a;
+      r += b;
+    }
+  }
+  const int njobs = __shfl(j, 63, 64);
+  if (block == 0) {  // for the merge
+    if (lane < P.b) P.seq_parts[lane] = make_int2(parts, r - prows);
+    const int any = __shfl(r, 63, 64);
+    if (lane == 0) P.head[1] = any > 0;
+  }
+  const int x = block % ATTN_XCDS, job = (int)((long long)njobs * x / ATTN_XCDS) + block / ATTN_XCDS;
+  ChunkJob out = {-1, 0, make_int2(1, 0)};
+  if (job >= (int)((long long)njobs * (x + 1) / ATTN_XCDS)) return out;
+  const unsigned long long past = __builtin_amdgcn_ballot_w64(j > job);
+  out.seq = __builtin_ctzll(past);
+  out.rel = job - __shfl(j - jobs, out.seq, 64);
+  out.sp = make_int2(__shfl(parts, out.seq, 64), __shfl(r - prows, out.seq, 64));
+  return out;
+}
+
 template <typename T, int DH>
-__device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel) {
+__device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int KEYS = ChunkTile<T>::KEYS, NST = KEYS / 32;
   constexpr int CH = DH * (int)sizeof(T) / 16;  // 16-byte pieces of a row
@@ -159,10 +243,8 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   const int lr = lane & 31, lk = lane >> 5;
   const int G = P.H / P.Hkv, QPT = 128 / G;
   const ChunkSeq S = chunk_seq(P, seq);
-  const int2 sp = P.seq_parts[seq];
   const int ntile = (S.m + QPT - 1) / QPT;
   const int part = rel % sp.x, tile = ntile - 1 - (rel / sp.x) % ntile, g = rel / sp.x / ntile;
-  const int slot = sp.x > 1 ? sp.y + rel : -1;
 
   const int qrow = wave * 32 + lr;
   const int pl = qrow / G, h = g * G + (qrow - pl * G);
@@ -435,16 +517,17 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
     vcur = vnext;
   }
 
-  if (slot >= 0) {  // a part: unnormalized sums and (max, sum) per row
+  if (sp.x > 1) {  // a part: unnormalized sums and (max, sum) per row
     if (!qvalid) return;
-    float* po = P.part_o + ((size_t)slot * 128 + qrow) * DH;
+    const size_t prow = (size_t)sp.y + (size_t)rel * (min(S.m, QPT) * G) + qrow;
+    float* po = P.part_o + prow * DH;
 #pragma unroll
     for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
       for (int v4 = 0; v4 < 4; ++v4)
         *(float4*)(po + dt * 32 + 8 * v4 + 4 * lk) =
             make_float4(o[dt][4 * v4 + 0], o[dt][4 * v4 + 1], o[dt][4 * v4 + 2], o[dt][4 * v4 + 3]);
-    if (lk == 0) *(float2*)(P.part_ml + ((size_t)slot * 128 + qrow) * 2) = make_float2(m_run, l_run);
+    if (lk == 0) *(float2*)(P.part_ml + prow * 2) = make_float2(m_run, l_run);
     return;
   }
   if (!qvalid) return;
@@ -464,53 +547,81 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   if (P.lse && lk == 0) P.lse[row * P.H + h] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
 }
 
-// Jobs from the XCD's queue, then from the next XCDs': a share is a contiguous
-// range of jobs, and every workgroup leaves once all eight are drained.
-template <typename T, int DH>
-__global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P) {
-  __shared__ int2 job_s;
+// INLINE (at most 64 sequences, fewer (tile, head) pairs than the grid): the job of
+// this workgroup by its own division.  Otherwise the division of chunk_plan_kernel:
+// one job a workgroup where they fit the grid, else jobs from the XCD's queue, then
+// from the next XCDs', until all eight are drained.
+template <typename T, int DH, bool INLINE>
+__global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P, int res) {
+  __shared__ ChunkJob job_s;
   const int lane = threadIdx.x & 63;
-  const int njobs = P.head[0];
-  int drained = 0;
-  for (;;) {
-    __syncthreads();  // every thread has finished the previous job and read job_s
+  if constexpr (INLINE) {
     if (threadIdx.x < 64) {
+      const ChunkJob j = chunk_wave_plan(P, ChunkTile<T>::KEYS, res, blockIdx.x);
+      if (lane == 0) job_s = j;
+    }
+  }
+  const int njobs = INLINE ? 0 : P.head[0];
+  const bool queue = njobs > (int)gridDim.x;
+  for (bool first = true;; first = false) {
+    if (!first) {
+      if (!queue) break;
+      __syncthreads();  // every thread has finished the previous job and read job_s
+    }
+    if (!INLINE && threadIdx.x < 64) {
       int job = -1;
-      while (drained < ATTN_XCDS) {
-        const int x = (blockIdx.x + drained) % ATTN_XCDS;
-        const int end = (int)((long long)njobs * (x + 1) / ATTN_XCDS);
-        int j = 0;
-        if (lane == 0) j = atomicAdd(&P.head[8 + x], 1);
-        j = __builtin_amdgcn_readfirstlane(j);
-        if (j < end) {
-          job = j;
-          break;
+      if (!queue) {
+        const int x = blockIdx.x % ATTN_XCDS;
+        job = (int)((long long)njobs * x / ATTN_XCDS) + blockIdx.x / ATTN_XCDS;
+        if (job >= (int)((long long)njobs * (x + 1) / ATTN_XCDS)) job = -1;
+      } else {
+        for (;;) {
+          // the first XCD from this one on whose queue has not been seen empty
+          const int x = (blockIdx.x + lane) % ATTN_XCDS;
+          const int end = (int)((long long)njobs * (x + 1) / ATTN_XCDS);
+          const int at = lane < ATTN_XCDS ? __hip_atomic_load(&P.head[8 + x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+          const unsigned long long some = __builtin_amdgcn_ballot_w64(lane < ATTN_XCDS && at < end);
+          if (!some) break;
+          const int l = __builtin_ctzll(some);
+          int j = 0;
+          if (lane == l) j = atomicAdd(&P.head[8 + x], 1);
+          j = __shfl(j, l, 64);
+          if (j < __shfl(end, l, 64)) {
+            job = j;
+            break;
+          }
         }
-        ++drained;
       }
-      int2 r = make_int2(-1, 0);
+      ChunkJob r = {-1, 0, make_int2(1, 0)};
       if (job >= 0) {
-        r.x = wave_find(P.job_base, P.b, job, lane);
-        r.y = job - P.job_base[r.x];
+        r.seq = wave_find(P.job_base, P.b, job, lane);
+        r.rel = job - P.job_base[r.seq];
+        r.sp = P.seq_parts[r.seq];
       }
       if (lane == 0) job_s = r;
     }
     __syncthreads();
-    const int2 r = job_s;
-    if (r.x < 0) break;
-    chunk_job<T, DH>(P, __builtin_amdgcn_readfirstlane(r.x), __builtin_amdgcn_readfirstlane(r.y));
+    const ChunkJob r = job_s;
+    if (r.seq < 0) break;
+    chunk_job<T, DH>(P, __builtin_amdgcn_readfirstlane(r.seq), __builtin_amdgcn_readfirstlane(r.rel),
+                     make_int2(__builtin_amdgcn_readfirstlane(r.sp.x), __builtin_amdgcn_readfirstlane(r.sp.y)));
+    if (INLINE) break;
   }
 }
 
-// Merge of divided tiles: a workgroup takes rows in turn, a thread 8 dimensions of a head.
+// Merge of divided tiles: a wave per (row, head), its lanes 64 / C8 parts at a time x
+// 8 dimensions each.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(ChunkArgs P) {
   if (P.head[1] == 0) return;
-  constexpr int C8 = DH / 8;
-  const int lane = threadIdx.x & 63;
+  constexpr int C8 = DH / 8, PG = 64 / C8;
+  const int lane = threadIdx.x & 63, c8 = lane % C8, pg = lane / C8;
   const int G = P.H / P.Hkv, QPT = 128 / G;
-  for (int r = blockIdx.x; r < P.rows; r += gridDim.x) {
-    if (r < P.row_start[0] || r >= P.row_start[P.b]) continue;
+  const int last = min(P.row_start[P.b], P.rows);
+  for (long long it = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); it < (long long)P.rows * P.H;
+       it += (long long)gridDim.x * 4) {
+    const int r = (int)(it / P.H), h = (int)(it % P.H), g = h / G;
+    if (r < P.row_start[0] || r >= last) continue;
     const int i = __builtin_amdgcn_readfirstlane(wave_find(P.row_start, P.b, r, lane));
     const int2 sp = P.seq_parts[i];
     if (sp.x <= 1) continue;
@@ -518,65 +629,99 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(ChunkArgs P) {
     const int j = r - S.r0;
     if (j >= S.m) continue;
     const int ntile = (S.m + QPT - 1) / QPT, tile = j / QPT, pl = j - tile * QPT;
-    for (int idx = threadIdx.x; idx < P.H * C8; idx += 256) {
-      const int h = idx / C8, c8 = idx % C8, g = h / G;
-      const size_t s0 = (size_t)sp.y + (size_t)(g * ntile + (ntile - 1 - tile)) * sp.x;
-      const int qrow = pl * G + (h - g * G);
-      float mx = -INFINITY;
-      for (int p = 0; p < sp.x; ++p) mx = fmaxf(mx, P.part_ml[((s0 + p) * 128 + qrow) * 2]);
-      const float mu = mx == -INFINITY ? 0.f : mx;
-      float l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int p = 0; p < sp.x; ++p) {
-        const size_t sr = (s0 + p) * 128 + qrow;
-        const float2 ml = *(const float2*)(P.part_ml + sr * 2);
-        const float w = __builtin_amdgcn_exp2f(ml.x - mu);
-        const float4 a = *(const float4*)(P.part_o + sr * DH + c8 * 8);
-        const float4 b = *(const float4*)(P.part_o + sr * DH + c8 * 8 + 4);
-        if (ml.y == 0.f) continue;  // nothing attended in this part
-        l += ml.y * w;
-        acc[0] += a.x * w;
-        acc[1] += a.y * w;
-        acc[2] += a.z * w;
-        acc[3] += a.w * w;
-        acc[4] += b.x * w;
-        acc[5] += b.y * w;
-        acc[6] += b.z * w;
-        acc[7] += b.w * w;
-      }
-      const float inv_l = l == 0.f ? 0.f : 1.0f / l;
-      T* op = (T*)P.O + ((size_t)r * P.H + h) * DH + c8 * 8;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) op[e] = Act<T>::from_f32(acc[e] * inv_l);
-      if (P.lse && c8 == 0) P.lse[(size_t)r * P.H + h] = l == 0.f ? -INFINITY : (mu + log2f(l)) * LN2;
+    const int R = min(S.m, QPT) * G;  // rows of a part
+    const size_t s0 = (size_t)sp.y + (size_t)(g * ntile + (ntile - 1 - tile)) * sp.x * R + pl * G + (h - g * G);
+    const float2* ml = (const float2*)P.part_ml + s0;
+    float mx = -INFINITY;
+    for (int p = lane; p < sp.x; p += 64) mx = fmaxf(mx, ml[(size_t)p * R].x);
+    mx = wave_max(mx);
+    const float mu = mx == -INFINITY ? 0.f : mx;
+    float l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float* po = P.part_o + s0 * DH + c8 * 8;
+    for (int p = pg; p < sp.x; p += PG) {
+      const float2 q = ml[(size_t)p * R];
+      const float4 a = *(const float4*)(po + (size_t)p * R * DH);
+      const float4 b = *(const float4*)(po + (size_t)p * R * DH + 4);
+      if (q.y == 0.f) continue;  // nothing attended in this part
+      const float w = __builtin_amdgcn_exp2f(q.x - mu);
+      l += q.y * w;
+      acc[0] += a.x * w;
+      acc[1] += a.y * w;
+      acc[2] += a.z * w;
+      acc[3] += a.w * w;
+      acc[4] += b.x * w;
+      acc[5] += b.y * w;
+      acc[6] += b.z * w;
+      acc[7] += b.w * w;
     }
+#pragma unroll
+    for (int o = C8; o < 64; o <<= 1) {
+      l += __shfl_xor(l, o, 64);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+    }
+    if (pg != 0) continue;
+    const float inv_l = l == 0.f ? 0.f : 1.0f / l;
+    T* op = (T*)P.O + ((size_t)r * P.H + h) * DH + c8 * 8;
+    if constexpr (sizeof(T) == 2) {
+      *(uint4*)op = make_uint4(pack_bf16x2(acc[0] * inv_l, acc[1] * inv_l), pack_bf16x2(acc[2] * inv_l, acc[3] * inv_l),
+                               pack_bf16x2(acc[4] * inv_l, acc[5] * inv_l), pack_bf16x2(acc[6] * inv_l, acc[7] * inv_l));
+    } else {
+      *(float4*)op = make_float4(acc[0] * inv_l, acc[1] * inv_l, acc[2] * inv_l, acc[3] * inv_l);
+      *(float4*)(op + 4) = make_float4(acc[4] * inv_l, acc[5] * inv_l, acc[6] * inv_l, acc[7] * inv_l);
+    }
+    if (P.lse && c8 == 0) P.lse[(size_t)r * P.H + h] = l == 0.f ? -INFINITY : (mu + log2f(l)) * LN2;
   }
+}
+
+// The kernels of a type and head dimension, allowed their two tile buffers of LDS on
+// the current device, and the workgroups of them that it holds (a multiple of the
+// XCDs; 0 when the runtime cannot tell), asked once a device.
+struct ChunkKernels {
+  void (*queued)(ChunkArgs, int);
+  void (*inl)(ChunkArgs, int);
+  void (*combine)(ChunkArgs);
+  int res;
+};
+template <typename T, int DH>
+static ChunkKernels chunk_kernels() {
+  static std::atomic<int> known[64];  // workgroups of each device, 0: not asked yet
+  ChunkKernels k = {chunk_attn_kernel<T, DH, false>, chunk_attn_kernel<T, DH, true>, chunk_combine_kernel<T, DH>, 0};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return k;
+  k.res = known[dev].load();
+  if (k.res) return k;
+  const size_t lds = (size_t)512 * DH;
+  for (auto f : {k.queued, k.inl})
+    if (hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return k;
+  k.res = std::min(resident_workgroups(k.queued, 256, lds), resident_workgroups(k.inl, 256, lds)) / ATTN_XCDS * ATTN_XCDS;
+  known[dev].store(k.res);
+  return k;
 }
 
 hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) {
   const int G = a.H / a.Hkv, qpt = 128 / G;
   const int keys = dtype == SAS_BF16 ? 64 : 32;
   const size_t lds = (size_t)512 * a.dh;  // two buffers of K and V tiles
-  void (*kern)(ChunkArgs);
-  void (*comb)(ChunkArgs);
-  if (dtype == SAS_BF16) {
-    kern = a.dh == 128 ? chunk_attn_kernel<bf16_t, 128> : chunk_attn_kernel<bf16_t, 64>;
-    comb = a.dh == 128 ? chunk_combine_kernel<bf16_t, 128> : chunk_combine_kernel<bf16_t, 64>;
-  } else {
-    kern = a.dh == 128 ? chunk_attn_kernel<float, 128> : chunk_attn_kernel<float, 64>;
-    comb = a.dh == 128 ? chunk_combine_kernel<float, 128> : chunk_combine_kernel<float, 64>;
-  }
-  const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
-  const int res = resident_workgroups(kern, 256, lds);
-  if (res <= 0) return hipErrorInvalidValue;
-  // the most jobs that there can be: tiles of every sequence, in parts of the least length
+  // (tile, kv head) pairs, at most
   const long long tiles = ((long long)a.rows / qpt + std::min(a.b, a.rows)) * a.Hkv;
-  const long long max_keys = std::min((long long)a.max_pages << a.ps_shift, 0x7fffffffll);
-  const long long parts = a.part_slots > 0 ? (max_keys + (long long)keys * CHUNK_MIN_TILES - 1) / ((long long)keys * CHUNK_MIN_TILES) : 1;
-  const long long most = parts < res ? tiles * parts : res;
-  chunk_plan_kernel<<<1, 1024, 0, s>>>(a, keys, res);
-  kern<<<(unsigned)std::min<long long>(res, most), 256, lds, s>>>(a);
-  if (a.part_slots > 0) comb<<<(unsigned)std::min(a.rows, 2048), 256, 0, s>>>(a);
+  ChunkKernels k;
+  if (dtype == SAS_BF16) k = a.dh == 128 ? chunk_kernels<bf16_t, 128>() : chunk_kernels<bf16_t, 64>();
+  else k = a.dh == 128 ? chunk_kernels<float, 128>() : chunk_kernels<float, 64>();
+  const int res = k.res;
+  if (res <= 0) return hipErrorInvalidValue;
+  // the most jobs that there can be: tiles in parts of the least length
+  const long long max_keys = (long long)a.max_pages << a.ps_shift;
+  const long long part_keys = (long long)keys * CHUNK_MIN_TILES;
+  const long long parts = a.part_rows > 0 ? (max_keys + part_keys - 1) / part_keys : 1;
+  const long long most = (std::min<long long>(res, tiles * std::min<long long>(parts, res)) + ATTN_XCDS - 1) / ATTN_XCDS * ATTN_XCDS;
+  const bool inl = a.b <= 64 && tiles < res;
+  if (!inl) chunk_plan_kernel<<<1, 1024, 0, s>>>(a, keys, res);
+  (inl ? k.inl : k.queued)<<<(unsigned)most, 256, lds, s>>>(a, res);
+  if (parts > 1) {
+    const long long waves = (long long)a.rows * a.H;
+    k.combine<<<(unsigned)std::min<long long>((waves + 3) / 4, 8192), 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -437,14 +437,15 @@ struct ChunkArgs {
   // scratch: the division of the work, written by the launch's first kernel
   int32_t* head;           // [16]
   int32_t* job_base;       // [b] first job of each sequence
-  int2* seq_parts;         // [b] parts of its tiles, first slot
-  float* part_o;           // [part_slots, 128, dh]
-  float* part_ml;          // [part_slots, 128, 2]
-  long long part_slots;    // 0: no tile is divided
+  int2* seq_parts;         // [b] parts of its tiles, first row of its parts
+  float* part_o;           // [part_rows, dh]
+  float* part_ml;          // [part_rows, 2]
+  long long part_rows;     // 0: no tile is divided
 };
-// Parts that a call works best with: twice the workgroups that the chip holds, which is
-// the most that parts of the average work of a workgroup can come to.
-constexpr long long CHUNK_PART_SLOTS = 1024;
+// Rows of parts that a call works best with: twice the workgroups that the chip holds,
+// which is the most that parts of the average work of a workgroup can come to, of 128
+// rows.
+constexpr long long CHUNK_PART_ROWS = 1024 * 128;
 constexpr int CHUNK_MIN_TILES = 2;  // key tiles of the least part
 constexpr long long CHUNK_MAX_KEYS = 1ll << 30;  // positions that a block table may cover
 hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s);
@@ -458,7 +459,7 @@ struct VerifyArgs {
   int32_t *out, *accepted;         // [b, max_draft + 1], [b]
   double* part;                    // [b, VERIFY_PIECES, 2] sums of the pieces of the weights
 };
-constexpr int VERIFY_PIECES = 32;
+constexpr int VERIFY_PIECES = 256, VERIFY_MIN_PIECES = 32;
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s);
 
 // ---- model_ends.hip --------------------------------------------------------

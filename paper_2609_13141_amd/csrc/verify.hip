@@ -7,9 +7,9 @@
 // itself when nothing is left), from p after the last when all were.
 //
 // Only one row of p and one of q are read in full, b vocab (4 or 8) bytes:
-// verify_sum_kernel cuts them into VERIFY_PIECES pieces, a workgroup each, and
-// leaves the pieces' sums; verify_pick_kernel finds the piece that the uniform
-// falls into and rescans that piece alone.  Differences and sums are fp64: the
+// verify_sum_kernel cuts them into pieces, a workgroup each, and leaves the pieces'
+// sums; verify_pick_kernel, a thread a piece, finds the one that the uniform falls
+// into by a prefix sum and rescans that piece alone, each thread a run of it.  Differences and sums are fp64: the
 // fp32 inputs' products and differences are exact there, and a token's border
 // in the CDF is some 1e-16 wide rather than the 1e-7 of an fp32 sum.
 #include "common.h"
@@ -96,73 +96,78 @@ __global__ void __launch_bounds__(VERIFY_NT) verify_sum_kernel(VerifyArgs P, int
   }
 }
 
-__global__ void __launch_bounds__(VERIFY_NT) verify_pick_kernel(VerifyArgs P, int len, int pieces) {
-  __shared__ double wsum[VERIFY_NT / 64];
-  __shared__ int found[2];  // the first token past the uniform, the last of any weight
-  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  VerifyRow v = verify_row(P, i);
-  const double* part = P.part + (size_t)i * pieces * 2;
-  double tot[2] = {0.0, 0.0};
-  for (int k = 0; k < pieces; ++k) {
-    tot[0] += part[2 * k];
-    tot[1] += part[2 * k + 1];
+// sum before this thread of v over the workgroup, and the whole (s: 4 values of LDS)
+__device__ __forceinline__ double scan_f64(double v, double* s, double& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
   }
-  const int which = tot[0] > 0.0 ? 0 : 1;  // nothing left over: the target itself
-  if (which == 1) {
+  __syncthreads();
+  if (lane == 63) s[wave] = x;
+  __syncthreads();
+  double at = 0.0, sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < VERIFY_NT / 64; ++w) {
+    if (w < wave) at += s[w];
+    sum += s[w];
+  }
+  total = sum;
+  x = __shfl_up(x, 1, 64);
+  return at + (lane ? x : 0.0);
+}
+
+__global__ void __launch_bounds__(VERIFY_NT) verify_pick_kernel(VerifyArgs P, int len, int pieces) {
+  __shared__ double s[VERIFY_NT / 64];
+  __shared__ int hit, some;  // the first piece or token past the uniform, the last of any weight
+  __shared__ double base_s[VERIFY_NT];
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const double* part = P.part + (size_t)i * pieces * 2;
+  const double w0 = tid < pieces ? part[2 * tid] : 0.0, w1 = tid < pieces ? part[2 * tid + 1] : 0.0;
+  VerifyRow v = verify_row(P, i);
+  if (tid == 0) {
+    hit = 0x7fffffff;
+    some = -1;
+  }
+  double left, all;
+  const double b0 = scan_f64(w0, s, left), b1 = scan_f64(w1, s, all);
+  if (!(left > 0.0)) {  // nothing left over: the target itself
     v.q = nullptr;
     v.skip = -1;
   }
-  const double aim = (double)P.u_sample[i] * tot[which];
-  // the first piece whose end lies past the aim (the last of any weight when none does)
-  int piece = -1, last = -1;
-  double before = 0.0, run = 0.0, lastb = 0.0;
-  for (int k = 0; k < pieces && piece < 0; ++k) {
-    const double w = part[2 * k + which];
-    if (w > 0.0) {
-      last = k;
-      lastb = run;
-    }
-    if (run + w > aim) {
-      piece = k;
-      before = run;
-    }
-    run += w;
-  }
-  if (piece < 0) {
-    piece = last;
-    before = lastb;
-  }
-  if (tid == 0) {
-    found[0] = 0x7fffffff;
-    found[1] = -1;
+  const double w = left > 0.0 ? w0 : w1, before = left > 0.0 ? b0 : b1;
+  const double aim = (double)P.u_sample[i] * (left > 0.0 ? left : all);
+  base_s[tid] = before;
+  if (w > 0.0) {
+    if (before + w > aim) atomicMin(&hit, tid);
+    atomicMax(&some, tid);
   }
   __syncthreads();
+  const int piece = hit != 0x7fffffff ? hit : some;
+  __syncthreads();
+  if (tid == 0) {
+    hit = 0x7fffffff;
+    some = -1;
+  }
   if (piece >= 0) {
-    const int e0 = piece * len, e1 = min(e0 + len, P.vocab);
-    // 256 tokens at a time, in order
-    for (int b0 = e0; b0 < e1; b0 += VERIFY_NT) {
-      const int e = b0 + tid;
-      const double w = e < e1 ? verify_left(v, e, v.p[e], v.q ? v.q[e] : 0.f) : 0.0;
-      double x = w;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(x, o, 64);
-        if (lane >= o) x += y;
+    // thread t's run of the piece: len / 256 tokens
+    const int run = len / VERIFY_NT, e0 = piece * len + tid * run, e1 = min(e0 + run, P.vocab);
+    double sum = 0.0, total;
+    for (int e = e0; e < e1; ++e) sum += verify_left(v, e, v.p[e], v.q ? v.q[e] : 0.f);
+    double at = base_s[piece] + scan_f64(sum, s, total);
+    if (sum > 0.0) {
+      int first = 0x7fffffff, last = -1;
+      for (int e = e0; e < e1; ++e) {
+        const double x = verify_left(v, e, v.p[e], v.q ? v.q[e] : 0.f);
+        if (!(x > 0.0)) continue;
+        at += x;
+        if (first == 0x7fffffff && at > aim) first = e;
+        last = e;
       }
-      if (lane == 63) wsum[wave] = x;
-      __syncthreads();
-      double at = before, sum = 0.0;
-      for (int k = 0; k < VERIFY_NT / 64; ++k) {
-        if (k < wave) at += wsum[k];
-        sum += wsum[k];
-      }
-      if (w > 0.0) {
-        if (at + x > aim) atomicMin(&found[0], e);
-        atomicMax(&found[1], e);
-      }
-      before += sum;
-      __syncthreads();
-      if (found[0] != 0x7fffffff) break;
+      if (first != 0x7fffffff) atomicMin(&hit, first);
+      atomicMax(&some, last);
     }
   }
   __syncthreads();
@@ -171,16 +176,18 @@ __global__ void __launch_bounds__(VERIFY_NT) verify_pick_kernel(VerifyArgs P, in
   for (int j = tid; j < W; j += VERIFY_NT) {
     int t = -1;
     if (j < v.acc) t = P.tokens[r0 + j];
-    else if (j == v.acc) t = found[0] != 0x7fffffff ? found[0] : found[1];
+    else if (j == v.acc) t = hit != 0x7fffffff ? hit : some;
     P.out[(size_t)i * W + j] = t;
   }
   if (tid == 0) P.accepted[i] = v.acc;
 }
 
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s) {
-  // pieces of whole 256-token steps
-  const int steps = cdiv(a.vocab, VERIFY_NT), pieces = std::min(VERIFY_PIECES, steps);
-  const int len = cdiv(steps, pieces) * VERIFY_NT;
+  // pieces of whole 256-token steps, at most a thread of the second kernel each: enough
+  // workgroups to read the rows from the whole chip, and no more, since each looks the
+  // accepted tokens up first
+  const int steps = cdiv(a.vocab, VERIFY_NT), want = std::max(VERIFY_MIN_PIECES, std::min(VERIFY_PIECES, 2048 / a.b));
+  const int len = cdiv(steps, std::min(steps, want)) * VERIFY_NT, pieces = cdiv(a.vocab, len);
   verify_sum_kernel<<<dim3(pieces, a.b), VERIFY_NT, 0, s>>>(a, len);
   verify_pick_kernel<<<a.b, VERIFY_NT, 0, s>>>(a, len, pieces);
   return hipGetLastError();
