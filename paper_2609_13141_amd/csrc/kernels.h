@@ -409,7 +409,7 @@ struct QkArgs {
   void *dq, *dk;
   float *dgain_q, *dgain_k, *part;  // part [QK_BWD_GROUPS, 2, dh]
 };
-constexpr int QK_BWD_GROUPS = 1024;  // workgroups of the backward (partial sums of the gains' gradients)
+constexpr int QK_BWD_GROUPS = 768;  // workgroups of the backward (partial sums of the gains' gradients)
 hipError_t launch_qk_norm_rope(int dtype, const QkArgs& a, hipStream_t s);
 hipError_t launch_qk_norm_rope_backward(int dtype, const QkArgs& a, hipStream_t s);
 // Summaries of the blocks that positions ctx_len[i] .. kv_len[i] - 1 complete, from

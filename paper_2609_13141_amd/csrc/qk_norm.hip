@@ -15,15 +15,21 @@
 
 namespace sas {
 
-// 8 values from floats, rounded once
-template <typename T>
+// 8 values from floats, rounded once; STREAM: past the caches
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store8(T* p, const float* x) {
-  if constexpr (sizeof(T) == 2) {
-    *(uint4*)p = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                            pack_bf16x2(x[6], x[7]));
+  constexpr int N = sizeof(T) / 2;
+  u32x4_t u[N];
+  if constexpr (N == 1) {
+    u[0] = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
   } else {
-    *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
-    *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e / 4][e % 4] = __float_as_uint(x[e]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (STREAM) __builtin_nontemporal_store(u[i], (u32x4_t*)p + i);
+    else ((u32x4_t*)p)[i] = u[i];
   }
 }
 
@@ -41,9 +47,8 @@ __device__ __forceinline__ QkPair qk_pair(const QkArgs& P, int lane) {
   return r;
 }
 // cos and sin of the pair's angle: the fraction of a turn is taken in fp64
-template <int DH>
-__device__ __forceinline__ float2 qk_turn(const QkArgs& P, const QkPair& pr, int row) {
-  const double a = (double)P.pos[(size_t)pr.axis * P.rows + row] * pr.freq;
+__device__ __forceinline__ float2 qk_turn(const QkPair& pr, int pos) {
+  const double a = (double)pos * pr.freq;
   const float f = (float)(a - rint(a));
   float s, c;
   sincospif(2.f * f, &s, &c);
@@ -92,7 +97,8 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs P, int parts, 
     slot = P.slot[row];
     if (slot >= (long long)P.num_pages << P.ps_shift) slot = -1;
   }
-  const float2 t = qk_turn<DH>(P, qk_pair<DH>(P, lane), row);
+  const QkPair pr = qk_pair<DH>(P, lane);
+  const float2 t = qk_turn(pr, P.pos[(size_t)pr.axis * P.rows + row]);
   if (lane < DH / 2) turn_s[wave][lane] = t;
   wave_lds_fence();
   float cs[8], sn[8];
@@ -123,7 +129,7 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs P, int parts, 
       if (gain) {
         Vec8<T> ga, gb;
         load16(gain + d0, DH / 2, ga, gb);
-        const float r = 1.0f / sqrtf(ss * (1.0f / DH) + P.eps);
+        const float r = rsqrtf(ss * (1.0f / DH) + P.eps);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[e] = x[e] * r * ga.get(e);
@@ -153,12 +159,26 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs P, int parts, 
 
 // Backward.  With dn the rotated-back gradient (the rotation's transpose) and
 // r = rsqrt(mean x^2 + eps): dg += dn x r and dx = r (g dn - x r^2 mean(g dn x)).
-// A workgroup takes every QK_BWD_GROUPS-th set of four units; its lanes keep
-// the gains' gradients of their 16 dimensions in fp32 registers and leave one
-// sum per workgroup, added in a fixed order by qk_gain_sum_kernel.
+// As many workgroups as stay resident walk the units (a row's group of heads) in
+// runs of QK_RUN, so that a wave forms a row's angles once for several; it loads its
+// next unit before it computes the current one.  Lanes keep the
+// gains' gradients of their 16 dimensions in fp32 registers and leave one sum per
+// workgroup, added in a fixed order by qk_gain_sum_kernel.
+// Measured at 16384 rows of 32/32 heads of 128 (bf16; 805 MB): 196 us with 1024
+// workgroups of two units at a time and no loads ahead, 168 us with the 768 that are
+// resident, 162 us with the next unit's loads ahead, 160 us in runs of 2 (4: 167,
+// one run a wave: 180), 150 us (5.4 TB/s; a copy reaches 4.9) with stores past the
+// caches, which leave them to the loads.
+constexpr int QK_RUN = 2;
+template <typename T>
+struct QkBwdUnit {
+  Vec8<T> a, b, da, db;  // x and its upstream gradient, both halves
+  int row, h, pos;
+};
+
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) qk_norm_rope_bwd_kernel(QkArgs P, int parts, long long units) {
-  constexpr int LPH = DH / 16, HPP = 64 / LPH, PU = QK_PASSES / 2;
+  constexpr int LPH = DH / 16, HPP = 64 / LPH;
   __shared__ __align__(16) float2 turn_s[4][DH / 2];
   __shared__ float gain_s[4][2][DH];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -170,76 +190,90 @@ __global__ void __launch_bounds__(256) qk_norm_rope_bwd_kernel(QkArgs P, int par
   for (int w = 0; w < 2; ++w)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dg[w][e] = 0.f;
-  for (long long unit = (long long)blockIdx.x * 4 + wave; unit < units; unit += (long long)gridDim.x * 4) {
-    const int row = (int)(unit / parts), part = (int)(unit % parts);
-    const int h0 = part * PU * HPP + lane / LPH;
-    Vec8<T> a[PU], b[PU], da[PU], db[PU];
-#pragma unroll
-    for (int u = 0; u < PU; ++u) {
-      const int h = min(h0 + u * HPP, heads - 1);
-      const bool isq = h < P.H;
-      const T* src = isq ? (const T*)P.q + row * P.qs + (long long)h * DH : (const T*)P.k + row * P.ks + (long long)(h - P.H) * DH;
-      const T* dsrc = isq ? (const T*)P.dq_out + ((size_t)row * P.H + h) * DH
-                          : (const T*)P.dk_out + ((size_t)row * P.Hkv + (h - P.H)) * DH;
-      load16(src + d0, DH / 2, a[u], b[u]);
-      load16(dsrc + d0, DH / 2, da[u], db[u]);
+  // (a unit past the end loads the last one again)
+  auto load = [&](QkBwdUnit<T>& U, long long unit) {
+    unit = min(unit, units - 1);
+    U.row = (int)(unit / parts);
+    U.h = (int)(unit % parts) * HPP + lane / LPH;
+    const int h = min(U.h, heads - 1);
+    const bool isq = h < P.H;
+    const T* src = isq ? (const T*)P.q + U.row * P.qs + (long long)h * DH
+                       : (const T*)P.k + U.row * P.ks + (long long)(h - P.H) * DH;
+    const T* dsrc = isq ? (const T*)P.dq_out + ((size_t)U.row * P.H + h) * DH
+                        : (const T*)P.dk_out + ((size_t)U.row * P.Hkv + (h - P.H)) * DH;
+    U.pos = P.pos[(size_t)pr.axis * P.rows + U.row];
+    load16(src + d0, DH / 2, U.a, U.b);
+    load16(dsrc + d0, DH / 2, U.da, U.db);
+  };
+  const long long jump = ((long long)gridDim.x * 4 - 1) * QK_RUN;
+  long long unit = ((long long)blockIdx.x * 4 + wave) * QK_RUN;
+  QkBwdUnit<T> U, N;
+  int turned = -1;  // the row whose angles LDS holds
+  int left = QK_RUN;
+  load(U, unit);
+  while (unit < units) {
+    unit += 1;
+    if (--left == 0) {
+      unit += jump;
+      left = QK_RUN;
     }
-    const float2 t = qk_turn<DH>(P, pr, row);
-    wave_lds_fence();
-    if (lane < DH / 2) turn_s[wave][lane] = t;
-    wave_lds_fence();
-    float cs[8], sn[8];
+    load(N, unit);
+    if (U.row != turned) {
+      const float2 t = qk_turn(pr, U.pos);
+      wave_lds_fence();
+      if (lane < DH / 2) turn_s[wave][lane] = t;
+      wave_lds_fence();
+      turned = U.row;
+    }
+    const bool isq = U.h < P.H, live = U.h < heads;
+    float n0[8], n1[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float2 x = turn_s[wave][d0 + e];
-      cs[e] = x.x;
-      sn[e] = x.y;
+      const float y0 = U.da.get(e), y1 = U.db.get(e);
+      n0[e] = fmaf(y0, x.x, y1 * x.y);
+      n1[e] = fmaf(y1, x.x, -(y0 * x.y));
     }
+    const T* gain = (const T*)(isq ? P.gain_q : P.gain_k);
+    Vec8<T> ga, gb;
+    float ss = 0.f, sx = 0.f;
+    if (gain) load16(gain + d0, DH / 2, ga, gb);
 #pragma unroll
-    for (int u = 0; u < PU; ++u) {
-      const int h = h0 + u * HPP;
-      const bool isq = h < P.H, live = h < heads;
-      float n0[8], n1[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float y0 = da[u].get(e), y1 = db[u].get(e);
-        n0[e] = fmaf(y0, cs[e], y1 * sn[e]);
-        n1[e] = fmaf(y1, cs[e], -(y0 * sn[e]));
-      }
-      const T* gain = (const T*)(isq ? P.gain_q : P.gain_k);
-      Vec8<T> ga, gb;
-      float ss = 0.f, sx = 0.f;
-      if (gain) load16(gain + d0, DH / 2, ga, gb);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = a[u].get(e), y = b[u].get(e);
-        ss = fmaf(x, x, fmaf(y, y, ss));
-        if (gain) sx = fmaf(n0[e] * ga.get(e), x, fmaf(n1[e] * gb.get(e), y, sx));
-      }
-      ss = head_sum<DH>(ss);
-      sx = head_sum<DH>(sx);
-      if (gain) {
-        const float r = 1.0f / sqrtf(ss * (1.0f / DH) + P.eps);
-        const float k = r * r * sx * (1.0f / DH);
+    for (int e = 0; e < 8; ++e) {
+      const float x = U.a.get(e), y = U.b.get(e);
+      ss = fmaf(x, x, fmaf(y, y, ss));
+      if (gain) sx = fmaf(n0[e] * ga.get(e), x, fmaf(n1[e] * gb.get(e), y, sx));
+    }
+    ss = head_sum<DH>(ss);
+    sx = head_sum<DH>(sx);
+    if (gain) {
+      const float r = rsqrtf(ss * (1.0f / DH) + P.eps);
+      const float k = r * r * sx * (1.0f / DH);
+      auto gains = [&](float* g) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float x = a[u].get(e), y = b[u].get(e);
-          if (live) {
-            const float g0 = n0[e] * (x * r), g1 = n1[e] * (y * r);
-            dg[0][e] += isq ? g0 : 0.f;
-            dg[0][8 + e] += isq ? g1 : 0.f;
-            dg[1][e] += isq ? 0.f : g0;
-            dg[1][8 + e] += isq ? 0.f : g1;
-          }
-          n0[e] = r * fmaf(n0[e], ga.get(e), -(x * k));
-          n1[e] = r * fmaf(n1[e], gb.get(e), -(y * k));
+          g[e] = fmaf(n0[e], U.a.get(e) * r, g[e]);
+          g[8 + e] = fmaf(n1[e], U.b.get(e) * r, g[8 + e]);
         }
+      };
+      if (live) {
+        if (isq) gains(dg[0]);
+        else gains(dg[1]);
       }
-      if (!live) continue;
-      T* dst = isq ? (T*)P.dq + ((size_t)row * P.H + h) * DH + d0 : (T*)P.dk + ((size_t)row * P.Hkv + (h - P.H)) * DH + d0;
-      store8(dst, n0);
-      store8(dst + DH / 2, n1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = U.a.get(e), y = U.b.get(e);
+        n0[e] = r * fmaf(n0[e], ga.get(e), -(x * k));
+        n1[e] = r * fmaf(n1[e], gb.get(e), -(y * k));
+      }
     }
+    if (live) {
+      T* dst = isq ? (T*)P.dq + ((size_t)U.row * P.H + U.h) * DH + d0
+                   : (T*)P.dk + ((size_t)U.row * P.Hkv + (U.h - P.H)) * DH + d0;
+      store8<true>(dst, n0);
+      store8<true>(dst + DH / 2, n1);
+    }
+    U = N;
   }
   if (!P.part) return;
 #pragma unroll
@@ -264,6 +298,7 @@ __global__ void __launch_bounds__(256) qk_gain_sum_kernel(const float* part, int
   __shared__ double s[32][8];
   const int col = blockIdx.x * 8 + (threadIdx.x & 7), j = threadIdx.x >> 3;
   double v = 0.0;
+#pragma unroll 8
   for (int r = j; r < n; r += 32) v += (double)part[(size_t)r * 2 * dh + col];
   s[j][threadIdx.x & 7] = v;
   __syncthreads();
@@ -281,7 +316,7 @@ __global__ void __launch_bounds__(256) qk_gain_sum_kernel(const float* part, int
 // kv head) at a time, a lane dh / 64 dimensions.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) chunk_summary_kernel(BlockSumArgs P) {
-  constexpr int NJ = DH / 64, STEP = 16;
+  constexpr int NJ = DH / 64, STEP = 16;  // dimensions of a lane, rows loaded together (B >= 16)
   extern __shared__ __align__(16) unsigned char sum_lds[];
   int* const blk0 = (int*)sum_lds;  // [b] blocks completed before sequence i
   __shared__ int wsum[4];
@@ -332,27 +367,29 @@ __global__ void __launch_bounds__(256) chunk_summary_kernel(BlockSumArgs P) {
 #pragma unroll
     for (int e = 0; e < NJ; ++e) acc[e] = 0.0;
     const int32_t* trow = P.table + (size_t)i * P.max_pages;
-    for (int p0 = m * P.B; p0 < (m + 1) * P.B; p0 += STEP) {
-      // the step's rows are loaded together, from clamped addresses
-      const T* src[STEP];
-      bool ok[STEP];
+    for (int p0 = m * P.B; p0 < (m + 1) * P.B; p0 += 64) {
+      // lane l holds the page of position p0 + l (-1: none, or past the block); the rows
+      // are loaded STEP at a time, from clamped addresses
+      const int pi = (p0 + lane) >> P.ps_shift;
+      int page = trow[min(pi, P.max_pages - 1)];
+      if (pi >= P.max_pages || page >= P.num_pages || p0 + lane >= (m + 1) * P.B) page = -1;
+      for (int q0 = 0; q0 < 64 && p0 + q0 < (m + 1) * P.B; q0 += STEP) {
+        struct Row {
+          T v[NJ];
+        } row[STEP];
+        bool ok[STEP];
 #pragma unroll
-      for (int u = 0; u < STEP; ++u) {
-        const int pi = (p0 + u) >> P.ps_shift;
-        const int page = trow[min(pi, P.max_pages - 1)];
-        ok[u] = pi < P.max_pages && page >= 0 && page < P.num_pages;
-        src[u] = (const T*)P.k_pages + ((((size_t)(ok[u] ? page : 0) * P.Hkv + g) << P.ps_shift) + ((p0 + u) & psm)) * DH
-                 + lane * NJ;
+        for (int u = 0; u < STEP; ++u) {
+          const int pg = __shfl(page, q0 + u, 64);
+          ok[u] = pg >= 0;
+          row[u] = *(const Row*)((const T*)P.k_pages +
+                                 ((((size_t)max(pg, 0) * P.Hkv + g) << P.ps_shift) + ((p0 + q0 + u) & psm)) * DH + lane * NJ);
+        }
+#pragma unroll
+        for (int u = 0; u < STEP; ++u)
+#pragma unroll
+          for (int e = 0; e < NJ; ++e) acc[e] += ok[u] ? (double)Act<T>::to_f32(row[u].v[e]) : 0.0;
       }
-      float v[STEP][NJ];
-#pragma unroll
-      for (int u = 0; u < STEP; ++u)
-#pragma unroll
-        for (int e = 0; e < NJ; ++e) v[u][e] = Act<T>::to_f32(src[u][e]);
-#pragma unroll
-      for (int u = 0; u < STEP; ++u)
-#pragma unroll
-        for (int e = 0; e < NJ; ++e) acc[e] += ok[u] ? (double)v[u][e] : 0.0;
     }
     T r[NJ];
 #pragma unroll
@@ -393,7 +430,7 @@ hipError_t launch_qk_norm_rope(int dtype, const QkArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_qk_norm_rope_backward(int dtype, const QkArgs& a, hipStream_t s) {
-  const int hpp = 1024 / a.dh, parts = cdiv(a.H + a.Hkv, hpp * QK_PASSES / 2);
+  const int hpp = 1024 / a.dh, parts = cdiv(a.H + a.Hkv, hpp);
   const long long units = (long long)a.rows * parts;
   const int grid = (int)std::min<long long>(QK_BWD_GROUPS, (units + 3) / 4);
   if (dtype == SAS_BF16) {

@@ -21,18 +21,19 @@ constexpr int VERIFY_NT = 256;
 
 // The rows that sequence i's last token is drawn from, found by the first wave.
 struct VerifyRow {
-  int acc;          // accepted tokens
+  int r0, acc;      // first drafted token, accepted ones
   const float* p;   // target row
   const float* q;   // draft row, or null
   int skip;         // token that is left out (a draft without probabilities), or -1
 };
-__device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i) {
+// `known`: the accepted tokens, or -1 to find them
+__device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i, int known) {
   const int lane = threadIdx.x & 63;
   const int r0 = min(max(P.start[i], 0), P.rows);
   const int m = min(min(max(P.start[i + 1], r0), P.rows) - r0, P.max_draft);
   // 64 drafted tokens at a time; the first that is not accepted ends the search
-  int acc = m;
-  for (int j0 = 0; j0 < m; j0 += 64) {
+  int acc = known >= 0 ? known : m;
+  for (int j0 = 0; known < 0 && j0 < m; j0 += 64) {
     const int j = j0 + lane;
     bool ok = true;
     if (j < m) {
@@ -51,6 +52,7 @@ __device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i) {
     }
   }
   VerifyRow v;
+  v.r0 = r0;
   v.acc = acc;
   v.p = P.target + (size_t)(r0 + i + acc) * P.vocab;
   const bool stop = acc < m;
@@ -74,7 +76,8 @@ __device__ __forceinline__ double wave_sum_f64(double x) {
 __global__ void __launch_bounds__(VERIFY_NT) verify_sum_kernel(VerifyArgs P, int len) {
   __shared__ double red[2][VERIFY_NT / 64];
   const int i = blockIdx.y, piece = blockIdx.x;
-  const VerifyRow v = verify_row(P, i);
+  const VerifyRow v = verify_row(P, i, -1);
+  if (piece == 0 && threadIdx.x == 0) P.accepted[i] = v.acc;
   const int e0 = piece * len, e1 = min(e0 + len, P.vocab);
   double left = 0.0, all = 0.0;
   for (int e = e0 + threadIdx.x; e < e1; e += VERIFY_NT) {
@@ -126,7 +129,7 @@ __global__ void __launch_bounds__(VERIFY_NT) verify_pick_kernel(VerifyArgs P, in
   const int i = blockIdx.x, tid = threadIdx.x;
   const double* part = P.part + (size_t)i * pieces * 2;
   const double w0 = tid < pieces ? part[2 * tid] : 0.0, w1 = tid < pieces ? part[2 * tid + 1] : 0.0;
-  VerifyRow v = verify_row(P, i);
+  VerifyRow v = verify_row(P, i, P.accepted[i]);
   if (tid == 0) {
     hit = 0x7fffffff;
     some = -1;
@@ -172,14 +175,12 @@ __global__ void __launch_bounds__(VERIFY_NT) verify_pick_kernel(VerifyArgs P, in
   }
   __syncthreads();
   const int W = P.max_draft + 1;
-  const int r0 = min(max(P.start[i], 0), P.rows);
   for (int j = tid; j < W; j += VERIFY_NT) {
     int t = -1;
-    if (j < v.acc) t = P.tokens[r0 + j];
+    if (j < v.acc) t = P.tokens[v.r0 + j];
     else if (j == v.acc) t = hit != 0x7fffffff ? hit : some;
     P.out[(size_t)i * W + j] = t;
   }
-  if (tid == 0) P.accepted[i] = v.acc;
 }
 
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s) {

@@ -575,19 +575,34 @@ def lm_head_argmax(cfg: Config, h, gamma, w_lm, *, logits: bool = False, ws: Wor
 # `ws` each takes its scratch from torch's allocator, so that calls on several
 # streams, and captured ones, share none; a given Workspace is for one stream.
 
-def _need(name: str, t, dtype, shape, dev):
-    """t is a contiguous tensor of that type and shape on `dev` (-1: any size)."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev or t.dim() != len(shape) \
-            or any(w not in (-1, n) for n, w in zip(t.shape, shape)) or not t.is_contiguous():
-        got = f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}" if isinstance(t, torch.Tensor) \
-            else type(t).__name__
-        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name}: expected contiguous {dtype} {list(shape)} on {dev}, got {got}")
+def _refuse(name: str, what: str, t):
+    got = f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}" if isinstance(t, torch.Tensor) \
+        else type(t).__name__
+    raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name}: expected {what}, got {got}")
+
+
+def _need(name: str, t, dtype, shape: tuple, dev) -> int:
+    """The address of t, a contiguous tensor of that type and shape (-1: any size) on `dev`."""
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == dev and t.is_contiguous():
+        got = tuple(t.shape)
+        if got == shape or (len(got) == len(shape) and all(w in (-1, n) for n, w in zip(got, shape))):
+            return t.data_ptr()
+    _refuse(name, f"contiguous {dtype} {list(shape)} on {dev}", t)
 
 
 def _device(name: str, t):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name} is not a tensor on the GPU")
     return t.device
+
+
+def _call(dev, fn, *args):
+    """fn(*args, current stream of dev), with dev the current device."""
+    if torch.cuda.current_device() == dev.index:
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev.index)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev.index)))
 
 
 def _act(cfg: Config):
@@ -595,42 +610,41 @@ def _act(cfg: Config):
 
 
 def _scratch(ws: Workspace | None, nbytes: int, dev):
-    """(buffer to keep until the call has returned, its pointer, its size)."""
-    if nbytes == 0:
-        return None, None, 0
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=dev) if ws is None else ws.get(nbytes)[0]
-    return buf, _ptr(buf), buf.numel()
+    """Scratch to keep until the call has returned: from `ws`, or torch's allocator."""
+    if nbytes == 0:  # a configuration that the call will refuse
+        nbytes = 16
+    return torch.empty(nbytes, dtype=torch.uint8, device=dev) if ws is None else ws.get(nbytes)[0]
 
 
-def _need_cache(cfg: Config, cache: PagedCache, b: int, dev):
-    Hkv, dh = cfg.n_kv_heads, cfg.head_dim
-    _need("cache.k_pages", cache.k_pages, _act(cfg), (-1, Hkv, cache.page_size, dh), dev)
-    _need("cache.v_pages", cache.v_pages, _act(cfg), tuple(cache.k_pages.shape), dev)
-    _need("cache.block_table", cache.block_table, torch.int32, (b, -1), dev)
-    _need("cache.k_summary", cache.k_summary, _act(cfg), (b, Hkv, -1, dh), dev)
+def _cache_arg(cfg: Config, cache: PagedCache, b: int, dev) -> PagedKV:
+    Hkv, dh, act, ps = cfg.n_kv_heads, cfg.head_dim, _act(cfg), cache.page_size
+    k, v, t, s = cache.k_pages, cache.v_pages, cache.block_table, cache.k_summary
+    return PagedKV(_need("cache.k_pages", k, act, (-1, Hkv, ps, dh), dev),
+                   _need("cache.v_pages", v, act, tuple(k.shape), dev),
+                   _need("cache.block_table", t, torch.int32, (b, -1), dev),
+                   _need("cache.k_summary", s, act, (b, Hkv, -1, dh), dev), k.shape[0], ps, t.shape[1], s.shape[2])
 
 
-def _rows_of(cfg: Config, name: str, t, heads: int, rows: int, dev):
-    """Elements between the rows of head rows [rows, heads, dh], whose rows are contiguous."""
+def _heads_arg(cfg: Config, name: str, t, heads: int, rows: int, dev):
+    """Address of head rows [rows, heads, dh], and elements between the rows (each contiguous)."""
     dh = cfg.head_dim
-    if not isinstance(t, torch.Tensor) or t.dtype != _act(cfg) or t.device != dev or tuple(t.shape) != (rows, heads, dh) \
-            or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh):
-        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name}: expected {_act(cfg)} [{rows}, {heads}, {dh}] on {dev} with "
-                       "contiguous rows")
-    return t.stride(0) if rows > 1 else heads * dh
+    if not isinstance(t, torch.Tensor) or t.dtype != _act(cfg) or t.device != dev or tuple(t.shape) != (rows, heads, dh):
+        _refuse(name, f"{_act(cfg)} [{rows}, {heads}, {dh}] on {dev}", t)
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != dh):
+        _refuse(name, "rows of contiguous heads", t)
+    return t.data_ptr(), st[0] if rows > 1 else heads * dh
 
 
 def _rotary(cfg: Config, pos, gain_q, gain_k, sections, rows: int, dev) -> Rotary:
     sections = (cfg.head_dim // 2,) if sections is None else tuple(int(n) for n in sections)
     if not 1 <= len(sections) <= 3:
         raise SasError(SAS_ERR_INVALID_ARGUMENT, f"sections {sections}: 1 to 3 axes")
-    if isinstance(pos, torch.Tensor) and pos.dim() == 1:
-        pos = pos[None]
-    _need("pos", pos, torch.int32, (len(sections), rows), dev)
-    for name, g in (("gain_q", gain_q), ("gain_k", gain_k)):
-        if g is not None:
-            _need(name, g, _act(cfg), (cfg.head_dim,), dev)
-    return Rotary(_ptr(gain_q), _ptr(gain_k), _ptr(pos), len(sections), (C.c_int32 * 3)(*sections))
+    act, dh = _act(cfg), cfg.head_dim
+    shape = (rows,) if isinstance(pos, torch.Tensor) and pos.dim() == 1 and len(sections) == 1 else (len(sections), rows)
+    return Rotary(None if gain_q is None else _need("gain_q", gain_q, act, (dh,), dev),
+                  None if gain_k is None else _need("gain_k", gain_k, act, (dh,), dev),
+                  _need("pos", pos, torch.int32, shape, dev), len(sections), (C.c_int32 * 3)(*sections))
 
 
 def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free_count, rows: int) -> dict:
@@ -642,21 +656,24 @@ def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free
     dev = _device("ctx_len", ctx_len)
     b = ctx_len.numel()
     i32 = torch.int32
-    for name, t in (("ctx_len", ctx_len), ("new_len", new_len), ("pages_held", pages_held)):
-        _need(name, t, i32, (b,), dev)
-    _need("free_pages", free_pages, i32, (-1,), dev)
-    _need("free_count", free_count, i32, (1,), dev)
-    _need("cache.block_table", cache.block_table, i32, (b, -1), dev)
-    out = {"row_start": torch.empty(b + 1, dtype=i32, device=dev), "kv_len": torch.empty(b, dtype=i32, device=dev),
-           "seq": torch.empty(rows, dtype=i32, device=dev), "pos": torch.empty(rows, dtype=i32, device=dev),
-           "slot": torch.empty(rows, dtype=torch.int64, device=dev),
-           "pages_held": torch.empty(b, dtype=i32, device=dev), "free_count": torch.empty(1, dtype=i32, device=dev),
-           "missing": torch.empty(1, dtype=i32, device=dev)}
-    pi = PlanIn(_ptr(ctx_len), _ptr(new_len), _ptr(pages_held), _ptr(free_pages), _ptr(free_count),
-                free_pages.numel())
-    po = PlanOut(*[_ptr(out[f]) for f, _ in PlanOut._fields_])
-    with torch.cuda.device(dev):
-        _check(lib().sas_plan_chunk(b, rows, C.byref(pi), C.byref(cache.struct()), C.byref(po), _stream()))
+    table = cache.block_table
+    kv = PagedKV(None, None, _need("cache.block_table", table, i32, (b, -1), dev), None, cache.k_pages.shape[0],
+                 cache.page_size, table.shape[1], 0)
+    pi = PlanIn(_need("ctx_len", ctx_len, i32, (b,), dev), _need("new_len", new_len, i32, (b,), dev),
+                _need("pages_held", pages_held, i32, (b,), dev), _need("free_pages", free_pages, i32, (-1,), dev),
+                _need("free_count", free_count, i32, (1,), dev), free_pages.numel())
+    if rows <= 0:
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"rows {rows} must be positive")
+    # one allocation: 16-byte aligned pieces, the gaps dropped
+    gap = lambda n: -n % 4  # noqa: E731
+    row_start, _, kv_len, _, held, _, seq, _, pos, _, free, _, missing, _ = torch.empty(
+        2 * (rows + gap(rows)) + 2 * (b + gap(b)) + b + 1 + gap(b + 1) + 8, dtype=i32, device=dev).split(
+        [b + 1, gap(b + 1), b, gap(b), b, gap(b), rows, gap(rows), rows, gap(rows), 1, 3, 1, 3])
+    out = {"row_start": row_start, "kv_len": kv_len, "seq": seq, "pos": pos,
+           "slot": torch.empty(rows, dtype=torch.int64, device=dev), "pages_held": held, "free_count": free,
+           "missing": missing}
+    po = PlanOut(*[out[f].data_ptr() for f, _ in PlanOut._fields_])
+    _call(dev, lib().sas_plan_chunk, b, rows, C.byref(pi), C.byref(kv), C.byref(po))
     return out
 
 
@@ -666,15 +683,14 @@ def qk_norm_rope(cfg: Config, q, k, pos, gain_q=None, gain_k=None, *, sections=N
     gain_k [dh] (None: no norm), then the rotation by pos [axes, rows] int32 (or
     [rows]), sections[a] rotary pairs turning by axis a (None: all by one)."""
     dev = _device("q", q)
-    rows = q.shape[0]
-    qs, ks = _rows_of(cfg, "q", q, cfg.n_heads, rows, dev), _rows_of(cfg, "k", k, cfg.n_kv_heads, rows, dev)
+    rows, H, Hkv, dh = q.shape[0], cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
+    (qp, qs), (kp, ks) = _heads_arg(cfg, "q", q, H, rows, dev), _heads_arg(cfg, "k", k, Hkv, rows, dev)
     rot = _rotary(cfg, pos, gain_q, gain_k, sections, rows, dev)
-    qo = torch.empty(rows, cfg.n_heads, cfg.head_dim, dtype=q.dtype, device=dev)
-    ko = torch.empty(rows, cfg.n_kv_heads, cfg.head_dim, dtype=q.dtype, device=dev)
+    qo = torch.empty(rows, H, dh, dtype=q.dtype, device=dev)
+    ko = torch.empty(rows, Hkv, dh, dtype=q.dtype, device=dev)
     if rows:
-        with torch.cuda.device(dev):
-            _check(lib().sas_qk_norm_rope(C.byref(cfg), rows, C.byref(rot), C.byref(Qkv(_ptr(q), _ptr(k), None, qs, ks, 0)),
-                                          _ptr(qo), _ptr(ko), _stream()))
+        _call(dev, lib().sas_qk_norm_rope, C.byref(cfg), rows, C.byref(rot), C.byref(Qkv(qp, kp, None, qs, ks, 0)),
+              qo.data_ptr(), ko.data_ptr())
     return qo, ko
 
 
@@ -683,23 +699,20 @@ def qk_norm_rope_backward(cfg: Config, q, k, pos, d_q, d_k, gain_q=None, gain_k=
     """Gradients of qk_norm_rope's inputs from those of its outputs d_q, d_k:
     dq, dk and, for given gains, dgain_q / dgain_k [dh] fp32."""
     dev = _device("q", q)
-    rows = q.shape[0]
-    qs, ks = _rows_of(cfg, "q", q, cfg.n_heads, rows, dev), _rows_of(cfg, "k", k, cfg.n_kv_heads, rows, dev)
+    rows, H, Hkv, dh = q.shape[0], cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
+    (qp, qs), (kp, ks) = _heads_arg(cfg, "q", q, H, rows, dev), _heads_arg(cfg, "k", k, Hkv, rows, dev)
     rot = _rotary(cfg, pos, gain_q, gain_k, sections, rows, dev)
-    _need("d_q", d_q, q.dtype, (rows, cfg.n_heads, cfg.head_dim), dev)
-    _need("d_k", d_k, q.dtype, (rows, cfg.n_kv_heads, cfg.head_dim), dev)
+    dqp, dkp = _need("d_q", d_q, q.dtype, (rows, H, dh), dev), _need("d_k", d_k, q.dtype, (rows, Hkv, dh), dev)
     out = {"dq": torch.empty_like(d_q), "dk": torch.empty_like(d_k)}
     new = torch.empty if rows else torch.zeros
     for name, g in (("dgain_q", gain_q), ("dgain_k", gain_k)):
         if g is not None:
-            out[name] = new(cfg.head_dim, dtype=torch.float32, device=dev)
+            out[name] = new(dh, dtype=torch.float32, device=dev)
     if rows:
-        buf, wsp, wsn = _scratch(ws, workspace_size(cfg, OP_QK_BACKWARD, rows, 0), dev)
-        with torch.cuda.device(dev):
-            _check(lib().sas_qk_norm_rope_backward(
-                C.byref(cfg), rows, C.byref(rot), C.byref(Qkv(_ptr(q), _ptr(k), None, qs, ks, 0)), _ptr(d_q), _ptr(d_k),
-                _ptr(out["dq"]), _ptr(out["dk"]), _ptr(out.get("dgain_q")), _ptr(out.get("dgain_k")), wsp, wsn,
-                _stream()))
+        buf = _scratch(ws, workspace_size(cfg, OP_QK_BACKWARD, rows, 0), dev)
+        _call(dev, lib().sas_qk_norm_rope_backward, C.byref(cfg), rows, C.byref(rot),
+              C.byref(Qkv(qp, kp, None, qs, ks, 0)), dqp, dkp, out["dq"].data_ptr(), out["dk"].data_ptr(),
+              _ptr(out.get("dgain_q")), _ptr(out.get("dgain_k")), buf.data_ptr(), buf.numel())
     return out
 
 
@@ -710,23 +723,18 @@ def cache_append(cfg: Config, cache: PagedCache, q, k, v, pos, slot, ctx_len, kv
     keys, values and the summaries of the blocks that the chunk completes; returns
     the normed and rotated queries."""
     dev = _device("q", q)
-    rows, b = q.shape[0], ctx_len.numel()
-    H, Hkv = cfg.n_heads, cfg.n_kv_heads
-    qs, ks = _rows_of(cfg, "q", q, H, rows, dev), _rows_of(cfg, "k", k, Hkv, rows, dev)
-    vs = _rows_of(cfg, "v", v, Hkv, rows, dev)
+    rows, b, H, Hkv, dh = q.shape[0], ctx_len.numel(), cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
+    (qp, qs), (kp, ks) = _heads_arg(cfg, "q", q, H, rows, dev), _heads_arg(cfg, "k", k, Hkv, rows, dev)
+    vp, vs = _heads_arg(cfg, "v", v, Hkv, rows, dev)
     rot = _rotary(cfg, pos, gain_q, gain_k, sections, rows, dev)
-    _need("slot", slot, torch.int64, (rows,), dev)
-    _need("ctx_len", ctx_len, torch.int32, (b,), dev)
-    _need("kv_len", kv_len, torch.int32, (b,), dev)
-    _need_cache(cfg, cache, b, dev)
-    if w_gk is not None:
-        _need("w_gk", w_gk, q.dtype, (Hkv, cfg.head_dim, cfg.head_dim), dev)
-    qo = torch.empty(rows, H, cfg.head_dim, dtype=q.dtype, device=dev)
+    sp = _need("slot", slot, torch.int64, (rows,), dev)
+    cl, kl = _need("ctx_len", ctx_len, torch.int32, (b,), dev), _need("kv_len", kv_len, torch.int32, (b,), dev)
+    kv = _cache_arg(cfg, cache, b, dev)
+    wp = None if w_gk is None else _need("w_gk", w_gk, q.dtype, (Hkv, dh, dh), dev)
+    qo = torch.empty(rows, H, dh, dtype=q.dtype, device=dev)
     if rows:
-        with torch.cuda.device(dev):
-            _check(lib().sas_cache_append(
-                C.byref(cfg), b, rows, C.byref(rot), C.byref(Qkv(_ptr(q), _ptr(k), _ptr(v), qs, ks, vs)), _ptr(slot),
-                _ptr(ctx_len), _ptr(kv_len), _ptr(w_gk), C.byref(cache.struct()), _ptr(qo), _stream()))
+        _call(dev, lib().sas_cache_append, C.byref(cfg), b, rows, C.byref(rot), C.byref(Qkv(qp, kp, vp, qs, ks, vs)),
+              sp, cl, kl, wp, C.byref(kv), qo.data_ptr())
     return qo
 
 
@@ -737,22 +745,19 @@ def attention_chunk(cfg: Config, q, cache: PagedCache, row_start, kv_len, *, lse
     cache already.  o [rows, H, dh] (`out` when given; rows behind row_start[b] are
     not written) and lse [rows, H] fp32."""
     dev = _device("q", q)
-    rows, b = q.shape[0], kv_len.numel()
-    _need("q", q, _act(cfg), (rows, cfg.n_heads, cfg.head_dim), dev)
-    _need("row_start", row_start, torch.int32, (b + 1,), dev)
-    _need("kv_len", kv_len, torch.int32, (b,), dev)
-    _need_cache(cfg, cache, b, dev)
-    if out is not None:
-        _need("out", out, q.dtype, tuple(q.shape), dev)
+    rows, b, H = q.shape[0], kv_len.numel(), cfg.n_heads
+    qp = _need("q", q, _act(cfg), (rows, H, cfg.head_dim), dev)
+    rp = _need("row_start", row_start, torch.int32, (b + 1,), dev)
+    kl = _need("kv_len", kv_len, torch.int32, (b,), dev)
+    kv = _cache_arg(cfg, cache, b, dev)
     r = {"o": torch.empty_like(q) if out is None else out}
+    op = _need("out", r["o"], q.dtype, (rows, H, cfg.head_dim), dev)
     if lse:
-        r["lse"] = torch.empty(rows, cfg.n_heads, dtype=torch.float32, device=dev)
+        r["lse"] = torch.empty(rows, H, dtype=torch.float32, device=dev)
     if rows:
-        buf, wsp, wsn = _scratch(ws, workspace_size(cfg, OP_ATTENTION_CHUNK, b, rows), dev)
-        with torch.cuda.device(dev):
-            _check(lib().sas_attention_chunk(C.byref(cfg), b, rows, _ptr(q), _ptr(row_start), _ptr(kv_len),
-                                             C.byref(cache.struct()), _ptr(r["o"]), _ptr(r.get("lse")), wsp, wsn,
-                                             _stream()))
+        buf = _scratch(ws, workspace_size(cfg, OP_ATTENTION_CHUNK, b, rows), dev)
+        _call(dev, lib().sas_attention_chunk, C.byref(cfg), b, rows, qp, rp, kl, C.byref(kv), op,
+              r["lse"].data_ptr() if lse else None, buf.data_ptr(), buf.numel())
     return r
 
 
@@ -766,21 +771,19 @@ def verify_drafts(target, draft, tokens, draft_start, u_accept, u_sample, max_dr
     dev = _device("target", target)
     rows, b = tokens.numel(), u_sample.numel()
     f32, i32 = torch.float32, torch.int32
-    _need("target", target, f32, (rows + b, -1), dev)
+    if max_draft < 0:
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"max_draft {max_draft} is negative")
+    tp = _need("target", target, f32, (rows + b, -1), dev)
     V = target.shape[1]
-    if draft is not None:
-        _need("draft", draft, f32, (rows, V), dev)
-    _need("tokens", tokens, i32, (rows,), dev)
-    _need("draft_start", draft_start, i32, (b + 1,), dev)
-    _need("u_accept", u_accept, f32, (rows,), dev)
-    _need("u_sample", u_sample, f32, (b,), dev)
-    out = {"tokens": torch.empty(b, max(max_draft, 0) + 1, dtype=i32, device=dev),
+    dp = None if draft is None else _need("draft", draft, f32, (rows, V), dev)
+    vi = VerifyIn(tp, dp or None, _need("tokens", tokens, i32, (rows,), dev),
+                  _need("draft_start", draft_start, i32, (b + 1,), dev), _need("u_accept", u_accept, f32, (rows,), dev),
+                  _need("u_sample", u_sample, f32, (b,), dev))
+    out = {"tokens": torch.empty(b, max_draft + 1, dtype=i32, device=dev),
            "accepted": torch.empty(b, dtype=i32, device=dev)}
-    vi = VerifyIn(_ptr(target), _ptr(draft) if rows else None, *[_ptr(t) for t in (tokens, draft_start, u_accept, u_sample)])
-    buf, wsp, wsn = _scratch(ws, lib().sas_workspace_size(None, OP_VERIFY_DRAFTS, b, 0), dev)
-    with torch.cuda.device(dev):
-        _check(lib().sas_verify_drafts(b, rows, V, max_draft, C.byref(vi), _ptr(out["tokens"]), _ptr(out["accepted"]),
-                                       wsp, wsn, _stream()))
+    buf = _scratch(ws, lib().sas_workspace_size(None, OP_VERIFY_DRAFTS, b, 0), dev)
+    _call(dev, lib().sas_verify_drafts, b, rows, V, max_draft, C.byref(vi), out["tokens"].data_ptr(),
+          out["accepted"].data_ptr(), buf.data_ptr(), buf.numel())
     return out
 
 
