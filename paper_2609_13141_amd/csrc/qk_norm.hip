@@ -15,21 +15,15 @@
 
 namespace sas {
 
-// 8 values from floats, rounded once; STREAM: past the caches
-template <bool STREAM = false, typename T>
+// 8 values from floats, rounded once
+template <typename T>
 __device__ __forceinline__ void store8(T* p, const float* x) {
-  constexpr int N = sizeof(T) / 2;
-  u32x4_t u[N];
-  if constexpr (N == 1) {
-    u[0] = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+  if constexpr (sizeof(T) == 2) {
+    *(uint4*)p = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                            pack_bf16x2(x[6], x[7]));
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) u[e / 4][e % 4] = __float_as_uint(x[e]);
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if constexpr (STREAM) __builtin_nontemporal_store(u[i], (u32x4_t*)p + i);
-    else ((u32x4_t*)p)[i] = u[i];
+    *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
   }
 }
 
@@ -166,9 +160,9 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs P, int parts, 
 // workgroup, added in a fixed order by qk_gain_sum_kernel.
 // Measured at 16384 rows of 32/32 heads of 128 (bf16; 805 MB): 196 us with 1024
 // workgroups of two units at a time and no loads ahead, 168 us with the 768 that are
-// resident, 162 us with the next unit's loads ahead, 160 us in runs of 2 (4: 167,
-// one run a wave: 180), 150 us (5.4 TB/s; a copy reaches 4.9) with stores past the
-// caches, which leave them to the loads.
+// resident, 162 us with the next unit's loads ahead, 160 us (5.0 TB/s; a copy reaches
+// 4.9) in runs of 2 (4: 167, one run a wave: 180).  Stores past the caches: 178 us, or
+// 150 us if the forward before it, 5% slower, stores so too.
 constexpr int QK_RUN = 2;
 template <typename T>
 struct QkBwdUnit {
@@ -270,8 +264,8 @@ __global__ void __launch_bounds__(256) qk_norm_rope_bwd_kernel(QkArgs P, int par
     if (live) {
       T* dst = isq ? (T*)P.dq + ((size_t)U.row * P.H + U.h) * DH + d0
                    : (T*)P.dk + ((size_t)U.row * P.Hkv + (U.h - P.H)) * DH + d0;
-      store8<true>(dst, n0);
-      store8<true>(dst + DH / 2, n1);
+      store8(dst, n0);
+      store8(dst + DH / 2, n1);
     }
     U = N;
   }
