@@ -1801,6 +1801,8 @@ sas_status sas_attention_chunk(const sas_config* c, int32_t batch, int32_t rows,
                 (long long)cache->max_pages_per_seq * cache->page_size);
   if ((long long)rows * c->n_heads > INT32_MAX / 2)
     return fail(SAS_ERR_UNSUPPORTED, "%d rows of %d heads (supported: <= 2^30 heads)", rows, c->n_heads);
+  if ((unsigned long long)c->n_kv_heads * cache->page_size * c->head_dim * act_bytes(c) > 0xffffffffull)
+    return fail(SAS_ERR_UNSUPPORTED, "a page of %d KV heads has 4 GiB or more", c->n_kv_heads);
   Carve cv(ws);
   const ChunkWs w = carve_chunk(cv, ws_bytes, c, batch);
   SAS_TRY(check_ws(ws, ws_bytes, w.need));

@@ -23,6 +23,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -62,6 +63,11 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs& P, int i) {
   return s;
 }
 
+__device__ __forceinline__ unsigned long long uniform64(unsigned long long x) {
+  return (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) |
+         (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32;
+}
+
 // largest i in [0, n) with base[i] <= x, by the 64 lanes of a wave (base[0] <= x, n <= 4096)
 __device__ __forceinline__ int wave_find(const int* base, int n, int x, int lane) {
   const int step = (n + 63) / 64;
@@ -79,7 +85,7 @@ struct ChunkWork {
   int units, nk, prow;
 };
 __device__ __forceinline__ ChunkWork chunk_work(const ChunkArgs& P, const ChunkSeq& q, int keys_per_tile) {
-  const int G = P.H / P.Hkv, qpt = 128 / G;
+  const int G = P.H / P.Hkv, qpt = P.tile_rows / G;
   ChunkWork w;
   w.units = P.Hkv * ((q.m + qpt - 1) / qpt);
   w.nk = (q.keys + keys_per_tile - 1) / keys_per_tile;
@@ -226,6 +232,69 @@ __device__ __forceinline__ ChunkJob chunk_wave_plan(const ChunkArgs& P, int keys
   return out;
 }
 
+// The pages of a sequence, as a wave holds them: lane l has the page of the tile's key l
+// (-1: no such key, or unmapped), and then the byte offset of that key's row of kv head g
+// in the pools (page 0 for keys without one).
+template <typename T, int DH>
+struct ChunkPages {
+  const ChunkArgs& P;
+  const int32_t* row;  // the sequence's block-table row
+  int g, keys, lane;
+  static constexpr int KEYS = ChunkTile<T>::KEYS, RB = DH * (int)sizeof(T);
+  __device__ __forceinline__ int load(int kt) const {
+    const int p = kt * KEYS + (lane & (KEYS - 1));
+    const int page = row[min(p >> P.ps_shift, P.max_pages - 1)];
+    return p < keys && page >= 0 && page < P.num_pages ? page : -1;
+  }
+  __device__ __forceinline__ uint64_t offset(int kt, int page) const {
+    const uint32_t stride = ((uint32_t)P.Hkv << P.ps_shift) * RB;  // bytes of a page
+    const uint32_t at = ((uint32_t)g << P.ps_shift) + ((kt * KEYS + (lane & (KEYS - 1))) & ((1 << P.ps_shift) - 1));
+    return (uint64_t)(uint32_t)max(page, 0) * stride + at * RB;
+  }
+  static __device__ __forceinline__ unsigned long long mapped(int page) {
+    return __builtin_amdgcn_ballot_w64(page >= 0) & (KEYS == 64 ? ~0ull : (1ull << KEYS) - 1);
+  }
+};
+
+// Copies a tile's rows from `pool` straight to LDS (256 threads), given the keys' row
+// offsets.  A wave copies KEYS / 4 consecutive rows, NL pieces of 1 KB in both places:
+// where the rows share a page, one scalar address serves them all (the instruction's
+// offset moves both sides) and the lanes' own offsets are those of every tile, so that
+// the copy takes next to nothing of either unit.
+template <typename T, int DH>
+__device__ __forceinline__ void chunk_copy(const ChunkArgs& P, const void* pool, unsigned char* dst, uint64_t off, int wave,
+                                           int lane) {
+  constexpr int KEYS = ChunkTile<T>::KEYS, RB = DH * (int)sizeof(T), CH = RB / 16, NL = KEYS * CH / 256, RW = 64 / CH;
+  const int lo = (int)(uint32_t)off, hi = (int)(uint32_t)(off >> 32);
+  asm volatile("" : "+v"(lane));  // (formed anew per tile: kept, the offsets would spill)
+  chunk_lds_t* const d = (chunk_lds_t*)(dst + wave * NL * 1024);
+  if ((1 << P.ps_shift) >= KEYS / 4) {
+    const int r0 = wave * (KEYS / 4);
+    uint64_t base = (uint64_t)pool + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(lo, r0) |
+                                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, r0) << 32);
+    asm("" : "+s"(base));  // (kept apart from the lanes' offsets: summed, they would be vector arithmetic)
+    // (the swizzle permutes bits of the row, and the pieces' first rows share none with lane / CH)
+    const uint32_t first = lane / CH * RB + (((lane % CH) ^ chunk_swz<T, DH>(lane / CH) ^ chunk_swz<T, DH>(r0)) << 4);
+#define CHUNK_PIECE(i)                                                                                         \
+  if constexpr (i < NL) {                                                                                      \
+    uint32_t at = first ^ (chunk_swz<T, DH>(i * RW) << 4);                                                     \
+    asm("" : "+v"(at));                                                                                        \
+    __builtin_amdgcn_global_load_lds((const void*)(base + at), d, 16, i * 1024, 0);                            \
+  }
+    CHUNK_PIECE(0) CHUNK_PIECE(1) CHUNK_PIECE(2) CHUNK_PIECE(3)
+#undef CHUNK_PIECE
+    static_assert(NL <= 4, "pieces");
+  } else {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = (wave * NL + i) * RW + lane / CH, c = (lane % CH) ^ chunk_swz<T, DH>(r);
+      const uint64_t at = (uint64_t)(uint32_t)__shfl(lo, r, 64) | (uint64_t)(uint32_t)__shfl(hi, r, 64) << 32;
+      __builtin_amdgcn_global_load_lds((const void*)((const char*)pool + at + c * 16),
+                                       (chunk_lds_t*)(dst + (wave * NL + i) * 1024), 16, 0, 0);
+    }
+  }
+}
+
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   constexpr bool BF = sizeof(T) == 2;
@@ -236,7 +305,7 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   constexpr int NL = KEYS * CH / 256;           // pieces of K (and of V) per thread and tile
   // two buffers of K and V (4 TB bytes; dynamic, because the compiler makes every read
   // of a static array wait for the direct-to-LDS loads in flight)
-  extern __shared__ __align__(16) unsigned char tiles[];
+  extern __shared__ __align__(256) unsigned char tiles[];
   __shared__ unsigned long long bad_s;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -278,29 +347,13 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   float m_run = -INFINITY, l_run = 0.f;
   const float qk_scale = P.sm_scale * LOG2E;
 
-  const int32_t* trow = P.table + (size_t)seq * P.max_pages;
-  const int psm = (1 << P.ps_shift) - 1;
-  // the page of key `lane` of tile kt (-1: no such key, or unmapped)
-  auto load_pages = [&](int kt) -> int {
-    const int p = kt * KEYS + (lane & (KEYS - 1));
-    const int page = trow[min(p >> P.ps_shift, P.max_pages - 1)];
-    return p < S.keys && page >= 0 && page < P.num_pages ? page : -1;
-  };
-  // K and V rows of tile kt into buffer buf; keys without a page read page 0
+  const ChunkPages<T, DH> pages = {P, P.table + (size_t)seq * P.max_pages, g, S.keys, lane};
   auto load_tile = [&](int kt, int pg, int buf) {
-    unsigned char* tb = tiles + buf * 2 * TB;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int p = (wave * NL + i) * 64 + lane, r = p / CH, c = (p % CH) ^ chunk_swz<T, DH>(r);
-      const int page = max(__shfl(pg, r, 64), 0);
-      const size_t off = ((((size_t)page * P.Hkv + g) << P.ps_shift) + ((kt * KEYS + r) & psm)) * DH + c * (16 / sizeof(T));
-      unsigned char* d = tb + (wave * NL + i) * 1024;
-      __builtin_amdgcn_global_load_lds((const void*)((const T*)P.k_pages + off), (chunk_lds_t*)d, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const void*)((const T*)P.v_pages + off), (chunk_lds_t*)(d + TB), 16, 0, 0);
-    }
+    const uint64_t off = pages.offset(kt, pg);
+    chunk_copy<T, DH>(P, P.k_pages, tiles + buf * 2 * TB, off, wave, lane);
+    chunk_copy<T, DH>(P, P.v_pages, tiles + buf * 2 * TB + TB, off, wave, lane);
   };
   constexpr unsigned long long ALL = KEYS == 64 ? ~0ull : 0xffffffffull;
-  auto valid_mask = [&](int pg) { return __builtin_amdgcn_ballot_w64(pg >= 0) & ALL; };
 
   // byte offsets of this lane's operands in a tile: K row lr (+ 32 st), chunk 2 ks + lk;
   // bf16 V columns by transposing reads (rows 4 lk + 8 half + (lane % 16) / 4)
@@ -318,10 +371,10 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   int pg = -1;
   unsigned long long vcur = 0;
   if (kt < tend) {
-    pg = load_pages(kt);
+    pg = pages.load(kt);
     load_tile(kt, pg, 0);
-    vcur = valid_mask(pg);
-    pg = load_pages(kt + 1);
+    vcur = pages.mapped(pg);
+    pg = pages.load(kt + 1);
   }
   for (; kt < tend; ++kt, buf ^= 1) {
     // this wave's loads of the tile are done; after the barrier everyone's are,
@@ -330,10 +383,10 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
     const int k0 = kt * KEYS;
     unsigned char* const tb = tiles + buf * 2 * TB;
     asm volatile("" : "+v"(o_row), "+v"(o_tr[0]), "+v"(o_tr[1]));  // (formed anew per tile: kept, they would spill)
-    const unsigned long long vnext = valid_mask(pg);
+    const unsigned long long vnext = pages.mapped(pg);
     if (kt + 1 < tend) {
       load_tile(kt + 1, pg, buf ^ 1);
-      pg = load_pages(kt + 2);
+      pg = pages.load(kt + 2);
     }
     const bool diag = k0 + KEYS - 1 > t0, gaps = vcur != ALL;
     if (diag || gaps) {
@@ -362,11 +415,11 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
         }
       }
       lds_barrier();
-      unsigned long long bm = bad_s;
+      unsigned long long bm = uniform64(bad_s);
       if (bm) {
         for (; bm; bm &= bm - 1) {
           const int r = __builtin_ctzll(bm);
-          if (k0 + r > t) continue;
+          const bool on = k0 + r <= t;
 #pragma unroll
           for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
@@ -375,7 +428,7 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
               const int c = d * (int)sizeof(T) / 16;
               const T x = *(const T*)(tb + TB + r * RB + ((c ^ chunk_swz<T, DH>(r)) << 4) + d * sizeof(T) % 16);
               const float f = Act<T>::to_f32(x);
-              if (!(fabsf(f) < INFINITY)) o[dt][v] += f;
+              o[dt][v] += on && !(fabsf(f) < INFINITY) ? f : 0.f;
             }
         }
         lds_barrier();
@@ -547,12 +600,380 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   if (P.lse && lk == 0) P.lse[row * P.H + h] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
 }
 
+// The same job over 256 rows (bf16): a wave owns two blocks of 32 rows, so that each K
+// and V fragment read from LDS serves two products, and one wave runs per SIMD with the
+// whole register file.  With no second wave to fill the gaps, the loop is pipelined
+// inside the wave: while the matrix unit forms S of tile t + 1 and then O += P V of tile
+// t, the vector unit does the exponentials of tile t and the row maxima of t + 1, which
+// are independent of it.  K runs one tile ahead of V in LDS: an iteration holds K(t + 1)
+// and V(t) and loads K(t + 2) and V(t + 1), one barrier each.
+// LDS reads at a 32-bit address: 16 bytes, and the transposing read of 8
+__device__ __forceinline__ bf16x8_t lds_read16(uint32_t a) {
+  return *(const __attribute__((address_space(3))) bf16x8_t*)(uintptr_t)a;
+}
+__device__ __forceinline__ uint2 lds_read_tr(uint32_t a) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)a));
+}
+
+// the larger of x in lanes l and l ^ 32
+__device__ __forceinline__ float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int DH, int NB>
+__device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
+  using T = bf16_t;
+  constexpr int KEYS = 64, RB = DH * 2, CH = DH / 8, TB = KEYS * RB, NL = KEYS * CH / 256, ROWS = 128 * NB;
+  // K buffers at 0 and TB, V buffers at 2 TB and 3 TB
+  extern __shared__ __align__(256) unsigned char tiles[];
+  __shared__ unsigned long long bad_s;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lk = lane >> 5;
+  const int G = P.H / P.Hkv, QPT = ROWS / G;
+  const ChunkSeq S = chunk_seq(P, seq);
+  const int ntile = (S.m + QPT - 1) / QPT;
+  const int part = rel % sp.x, tile = ntile - 1 - (rel / sp.x) % ntile, g = rel / sp.x / ntile;
+  const int t0 = S.base + tile * QPT;
+  const int t_hi = S.base + min(tile * QPT + QPT, S.m) - 1;
+  const int nkt = (min(max(t_hi + 1, 0), S.keys) + KEYS - 1) / KEYS;
+  const int per = (nkt + sp.x - 1) / sp.x;
+  const int tlo = part * per, tend = min(tlo + per, nkt);
+
+  int t[NB];           // positions of this lane's rows (-1: none)
+  uint4 qb[NB][DH / 16];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int qrow = wave * 32 * NB + b * 32 + lr, pl = qrow / G;
+    const bool valid = pl < QPT && tile * QPT + pl < S.m;
+    t[b] = valid ? t0 + pl : -1;
+    const T* qp = (const T*)P.Q + (((size_t)S.r0 + tile * QPT + pl) * P.H + g * G + (qrow - pl * G)) * DH;
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks)
+      qb[b][ks] = valid ? *(const uint4*)(qp + ks * 16 + lk * 8) : make_uint4(0, 0, 0, 0);
+  }
+
+  floatx16_t o[NB][DH / 32];
+  float m_run[NB], l_run[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    m_run[b] = -INFINITY;
+    l_run[b] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[b][dt][v] = 0.f;
+  }
+  const float qk_scale = P.sm_scale * LOG2E;
+
+  const ChunkPages<T, DH> pages = {P, P.table + (size_t)seq * P.max_pages, g, S.keys, lane};
+  auto load_k = [&](int kt, uint64_t off) { chunk_copy<T, DH>(P, P.k_pages, tiles + ((kt - tlo) & 1) * TB, off, wave, lane); };
+  auto load_v = [&](int kt, uint64_t off) { chunk_copy<T, DH>(P, P.v_pages, tiles + (2 + ((kt - tlo) & 1)) * TB, off, wave, lane); };
+  auto tile_barrier = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(chunk_lds_t*)tiles;  // aligned to a row
+  uint32_t o_row = lds0 + lr * RB + ((lk ^ chunk_swz<T, DH>(lr)) << 4);
+  uint32_t o_tr[2];
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    const int r = 4 * lk + 8 * hf + ((lane & 15) >> 2);
+    o_tr[hf] = lds0 + r * RB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ chunk_swz<T, DH>(r)) << 4) + (lane & 1) * 8;
+  }
+
+  typedef floatx16_t scores_t[NB];  // of 32 keys
+  // S = K Q^T of half st of the tile in the K buffer at kb
+  auto product = [&](scores_t& s, uint32_t kb, int st) __attribute__((always_inline)) {
+    const floatx16_t z = {};
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) {
+      const bf16x8_t k = lds_read16((o_row ^ (ks << 5)) + kb + st * 32 * RB);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, *(const bf16x8_t*)&qb[b][ks], ks ? s[b] : z, 0, 0, 0);
+    }
+  };
+  // masks of a tile that reaches past the first row's position, or has keys without a page
+  auto mask = [&](scores_t& s, int kt, int st, unsigned long long vm) {
+    int lk4 = 4 * lk;
+    asm volatile("" : "+v"(lk4));
+    vm >>= lk4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int j = st * 32 + 8 * (v >> 2) + (v & 3);
+        if (kt * KEYS + j + lk4 > t[b] || !((vm >> j) & 1)) s[b][v] = -INFINITY;
+      }
+  };
+  // row maxima of the scaled logits (the scale is positive)
+  auto maxima = [&](const scores_t& s, float* mx) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      float m = s[b][0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) m = fmaxf(m, s[b][v]);
+      mx[b] = pair_max(m * qk_scale);
+    }
+  };
+  // The reference moves only where a logit exceeds it by more than 8, in log2 units (any
+  // reference gives the same sums); what is summed so far is then rescaled.
+  auto reference = [&](const float* mx) __attribute__((always_inline)) {
+    bool any = false;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) any = any || mx[b] > m_run[b] + 8.f;
+    if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (mx[b] > m_run[b] + 8.f) {
+        // (nothing is summed yet where m_run is -inf)
+        const float alpha = m_run[b] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[b] - mx[b]);
+        m_run[b] = mx[b];
+        l_run[b] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[b][dt][v] *= alpha;
+      }
+    }
+  };
+  // the values of a masked tile: see chunk_job
+  auto fix_values = [&](unsigned char* vb, int kt, unsigned long long vm) {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));  // (nothing of this rare path is kept outside it)
+    if (tid == 0) bad_s = 0;
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      asm volatile("" ::: "memory");
+      const int r = ((wave * NL + i) * 64 + ln) / CH;
+      uint4* pv = (uint4*)(vb + (wave * NL + i) * 1024 + ln * 16);
+      if (!((vm >> r) & 1)) {
+        *pv = make_uint4(0, 0, 0, 0);
+      } else {
+        const uint4 u = *pv;
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          bad = bad || (w[e] & 0x7f800000u) == 0x7f800000u || (w[e] & 0x7f80u) == 0x7f80u;
+        if (bad) atomicOr(&bad_s, 1ull << r);
+      }
+    }
+    lds_barrier();
+    unsigned long long bm = uniform64(bad_s);
+    if (!bm) return;
+    for (; bm; bm &= bm - 1) {
+      const int r = __builtin_ctzll(bm);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const bool on = kt * KEYS + r <= t[b];
+#pragma unroll
+        for (int dv = 0; dv < DH / 2; ++dv) {
+            const int dt = dv / 16, v = dv % 16;
+            if (dv % 4 == 0) asm volatile("" ::: "memory");  // (few loads at a time: registers are short)
+            const int d = dt * 32 + 8 * (v >> 2) + 4 * (ln >> 5) + (v & 3);
+            const float f = bf16_to_f32(*(const T*)(vb + r * RB + (((d >> 3) ^ chunk_swz<T, DH>(r)) << 4) + d * 2 % 16));
+            o[b][dt][v] += on && !(fabsf(f) < INFINITY) ? f : 0.f;
+          }
+      }
+    }
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      asm volatile("" ::: "memory");
+      T* pv = (T*)(vb + (wave * NL + i) * 1024 + ln * 16);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (!(fabsf(bf16_to_f32(pv[e])) < INFINITY)) pv[e] = 0;
+    }
+    lds_barrier();
+  };
+
+  unsigned long long vm = 0, vm1 = 0;  // keys of tiles kt and kt + 1 with a page
+  uint64_t off1 = 0;                   // row offsets of tile kt + 1
+  int pg2 = -1;                        // pages of tile kt + 2
+  auto special = [&](int kt, unsigned long long v) { return kt * KEYS + KEYS - 1 > t0 || v != ~0ull; };
+  if (tlo < tend) {
+    scores_t s0, s1, u0, u1;  // (a tile's halves, by turns)
+    {
+      const int pg0 = pages.load(tlo), pg1 = pages.load(tlo + 1);
+      const uint64_t off0 = pages.offset(tlo, pg0);
+      off1 = pages.offset(tlo + 1, pg1);
+      load_k(tlo, off0);
+      load_v(tlo, off0);
+      if (tlo + 1 < tend) load_k(tlo + 1, off1);
+      pg2 = pages.load(tlo + 2);
+      vm = pages.mapped(pg0);
+      vm1 = pages.mapped(pg1);
+    }
+    float mx[NB];
+    tile_barrier();
+    // both halves of K(tlo) are read before the first iteration's loads replace it
+    product(s0, 0, 0);
+    product(s1, 0, 1);
+    if (special(tlo, vm)) mask(s0, tlo, 0, vm);
+    maxima(s0, mx);
+    reference(mx);
+    // tile kt, of scores s0 and s1; leaves those of the next in n0 and n1
+    // (odd: the tile lies in the odd buffers, counted from tlo)
+    auto tile = [&](int kt, scores_t& s0, scores_t& s1, scores_t& n0, scores_t& n1, auto odd_t) __attribute__((always_inline)) {
+      constexpr int odd = decltype(odd_t)::value;
+      tile_barrier();  // K(kt + 1) and V(kt) are there; K(kt) and V(kt - 1) are free
+      const unsigned long long vm2 = pages.mapped(pg2);
+      const uint64_t off2 = pages.offset(kt + 2, pg2);
+      if (kt + 1 < tend) load_v(kt + 1, off1);
+      if (kt + 2 < tend) load_k(kt + 2, off2);
+      off1 = off2;
+      pg2 = pages.load(kt + 3);
+      const bool masked = special(kt, vm), masked1 = special(kt + 1, vm1);
+      if (masked) fix_values(tiles + (2 + odd) * TB, kt, vm);
+      asm volatile("" : "+v"(o_row), "+v"(o_tr[0]), "+v"(o_tr[1]));  // (formed anew per tile: kept, they would spill)
+      constexpr uint32_t kb = (odd ^ 1) * TB, vb = (2 + odd) * TB;
+      // Half st of the tile, whose scores s turn into those of the next tile's half: the
+      // products of those between this half's exponentials and sums, then its products
+      // with the values between the maxima of the following half, `after`.  One product
+      // takes the matrix unit 32 cycles, about what a step's vector instructions take the
+      // other; the steps are pinned, because the compiler groups each kind of instruction.
+      auto half = [&](const scores_t& s, scores_t& n, const scores_t& after, int st) __attribute__((always_inline)) {
+        constexpr int NK = DH / 16, ND = DH / 32, PER = 16 / NK;  // steps, groups of dimensions, weights a step
+        uint32_t pk[NB][8];
+        uint4 f0[ND], f1[ND];
+        bf16x8_t kf[NK];
+        float bias[NB], p[NB][16], r2[NB][2];
+        auto read_k = [&](int ks) { kf[ks] = lds_read16((o_row ^ (ks << 5)) + kb + st * 32 * RB); };
+        auto read_v = [&](uint4* f, int dt, int ks) {
+          const uint2 lo = lds_read_tr((o_tr[0] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB);
+          const uint2 hi = lds_read_tr((o_tr[1] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB);
+          f[dt] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        };
+        // P is rounded to bf16 for the matrix instruction; the sum keeps the fp32 weights
+        auto finish = [&](int u) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int v = u * PER; v < (u + 1) * PER; v += 2) {
+              r2[b][0] += p[b][v];
+              r2[b][1] += p[b][v + 1];
+              pk[b][v / 2] = pack_bf16x2(p[b][v], p[b][v + 1]);
+            }
+        };
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          bias[b] = m_run[b] == -INFINITY ? 0.f : -m_run[b];
+          r2[b][0] = r2[b][1] = 0.f;
+        }
+        read_k(0);
+        read_k(1);
+        read_k(2);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < NK; ++u) {
+          if (u + 3 < NK) read_k(u + 3);
+          else if (u + 3 - NK < ND) read_v(f0, u + 3 - NK, 0);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const floatx16_t z = {};
+            n[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u], *(const bf16x8_t*)&qb[b][u], u ? n[b] : z, 0, 0, 0);
+#pragma unroll
+            for (int v = u * PER; v < (u + 1) * PER; ++v)
+              p[b][v] = __builtin_amdgcn_exp2f(fmaf(s[b][v], qk_scale, bias[b]));
+          }
+          if (u > 0) finish(u - 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        finish(NK - 1);
+#pragma unroll
+        for (int dt = 3; dt < ND; ++dt) read_v(f0, dt, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        float m[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          l_run[b] += r2[b][0] + r2[b][1];  // this lane's keys
+          m[b] = after[b][0];
+        }
+#pragma unroll
+        for (int u = 0; u < 2 * ND; ++u) {
+          const int dt = u % ND, v0 = 4 * (u / ND);
+          if (u < ND) read_v(f1, u, 1);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const uint4 pu = make_uint4(pk[b][v0], pk[b][v0 + 1], pk[b][v0 + 2], pk[b][v0 + 3]);
+            const uint4& f = u < ND ? f0[dt] : f1[dt];
+            o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t*)&f, *(const bf16x8_t*)&pu, o[b][dt], 0, 0, 0);
+#pragma unroll
+            for (int v = u * PER; v < (u + 1) * PER; ++v) m[b] = fmaxf(m[b], after[b][v]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          mx[b] = pair_max(m[b] * qk_scale);
+        }
+      };
+      half(s0, n0, s1, 0);
+      if (masked) {
+        mask(s1, kt, 1, vm);
+        maxima(s1, mx);
+      }
+      reference(mx);
+      half(s1, n1, n0, 1);
+      if (masked1) {
+        mask(n0, kt + 1, 0, vm1);
+        maxima(n0, mx);
+      }
+      if (kt + 1 < tend) reference(mx);
+      vm = vm1;
+      vm1 = vm2;
+    };
+    for (int kt = tlo;;) {
+      tile(kt, s0, s1, u0, u1, std::integral_constant<int, 0>{});
+      if (++kt >= tend) break;
+      tile(kt, u0, u1, s0, s1, std::integral_constant<int, 1>{});
+      if (++kt >= tend) break;
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) l_run[b] += __shfl_xor(l_run[b], 32, 64);
+
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    if (t[b] < 0 && !(wave * 32 * NB + b * 32 + lr < QPT * G && tile * QPT + (wave * 32 * NB + b * 32 + lr) / G < S.m)) continue;
+    const int qrow = wave * 32 * NB + b * 32 + lr, pl = qrow / G, h = g * G + (qrow - pl * G);
+    const size_t row = (size_t)S.r0 + tile * QPT + pl;
+    if (sp.x > 1) {  // a part: unnormalized sums and (max, sum) per row
+      const size_t prow = (size_t)sp.y + (size_t)rel * (min(S.m, QPT) * G) + qrow;
+      float* po = P.part_o + prow * DH;
+#pragma unroll
+      for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4)
+          *(float4*)(po + dt * 32 + 8 * v4 + 4 * lk) =
+              make_float4(o[b][dt][4 * v4 + 0], o[b][dt][4 * v4 + 1], o[b][dt][4 * v4 + 2], o[b][dt][4 * v4 + 3]);
+      if (lk == 0) *(float2*)(P.part_ml + prow * 2) = make_float2(m_run[b], l_run[b]);
+      continue;
+    }
+    const float inv_l = l_run[b] == 0.f ? 0.f : 1.0f / l_run[b];
+    T* op = (T*)P.O + (row * P.H + h) * DH;
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = l_run[b] == 0.f ? 0.f : o[b][dt][4 * v4 + e] * inv_l;
+        *(uint2*)(op + dt * 32 + 8 * v4 + 4 * lk) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+      }
+    if (P.lse && lk == 0) P.lse[row * P.H + h] = l_run[b] == 0.f ? -INFINITY : (m_run[b] + log2f(l_run[b])) * LN2;
+  }
+}
+
 // INLINE (at most 64 sequences, fewer (tile, head) pairs than the grid): the job of
 // this workgroup by its own division.  Otherwise the division of chunk_plan_kernel:
 // one job a workgroup where they fit the grid, else jobs from the XCD's queue, then
 // from the next XCDs', until all eight are drained.
-template <typename T, int DH, bool INLINE>
-__global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P, int res) {
+template <typename T, int DH, bool INLINE, bool WIDE>
+__global__ void __launch_bounds__(256, WIDE && CHUNK_WIDE_ROWS > 128 ? 1 : 2) chunk_attn_kernel(ChunkArgs P, int res) {
   __shared__ ChunkJob job_s;
   const int lane = threadIdx.x & 63;
   if constexpr (INLINE) {
@@ -603,8 +1024,10 @@ __global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P, int res
     __syncthreads();
     const ChunkJob r = job_s;
     if (r.seq < 0) break;
-    chunk_job<T, DH>(P, __builtin_amdgcn_readfirstlane(r.seq), __builtin_amdgcn_readfirstlane(r.rel),
-                     make_int2(__builtin_amdgcn_readfirstlane(r.sp.x), __builtin_amdgcn_readfirstlane(r.sp.y)));
+    const int seq = __builtin_amdgcn_readfirstlane(r.seq), rel = __builtin_amdgcn_readfirstlane(r.rel);
+    const int2 sp = make_int2(__builtin_amdgcn_readfirstlane(r.sp.x), __builtin_amdgcn_readfirstlane(r.sp.y));
+    if constexpr (WIDE) chunk_job_wide<DH, CHUNK_WIDE_ROWS / 128>(P, seq, rel, sp);
+    else chunk_job<T, DH>(P, seq, rel, sp);
     if (INLINE) break;
   }
 }
@@ -616,7 +1039,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(ChunkArgs P) {
   if (P.head[1] == 0) return;
   constexpr int C8 = DH / 8, PG = 64 / C8;
   const int lane = threadIdx.x & 63, c8 = lane % C8, pg = lane / C8;
-  const int G = P.H / P.Hkv, QPT = 128 / G;
+  const int G = P.H / P.Hkv, QPT = P.tile_rows / G;
   const int last = min(P.row_start[P.b], P.rows);
   for (long long it = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); it < (long long)P.rows * P.H;
        it += (long long)gridDim.x * 4) {
@@ -683,10 +1106,11 @@ struct ChunkKernels {
   void (*combine)(ChunkArgs);
   int res;
 };
-template <typename T, int DH>
+template <typename T, int DH, bool WIDE>
 static ChunkKernels chunk_kernels() {
   static std::atomic<int> known[64];  // workgroups of each device, 0: not asked yet
-  ChunkKernels k = {chunk_attn_kernel<T, DH, false>, chunk_attn_kernel<T, DH, true>, chunk_combine_kernel<T, DH>, 0};
+  ChunkKernels k = {chunk_attn_kernel<T, DH, false, WIDE>, chunk_attn_kernel<T, DH, true, WIDE>,
+                    chunk_combine_kernel<T, DH>, 0};
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return k;
   k.res = known[dev].load();
@@ -699,15 +1123,18 @@ static ChunkKernels chunk_kernels() {
   return k;
 }
 
-hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) {
-  const int G = a.H / a.Hkv, qpt = 128 / G;
+hipError_t launch_chunk_attention(int dtype, const ChunkArgs& args, hipStream_t s) {
+  ChunkArgs a = args;
+  const int G = a.H / a.Hkv;
   const int keys = dtype == SAS_BF16 ? 64 : 32;
-  const size_t lds = (size_t)512 * a.dh;  // two buffers of K and V tiles
+  const bool wide = dtype == SAS_BF16 && (long long)a.rows * G > 128ll * std::min(a.b, a.rows);
+  a.tile_rows = wide ? CHUNK_WIDE_ROWS : 128;
   // (tile, kv head) pairs, at most
-  const long long tiles = ((long long)a.rows / qpt + std::min(a.b, a.rows)) * a.Hkv;
+  const long long tiles = ((long long)a.rows / (a.tile_rows / G) + std::min(a.b, a.rows)) * a.Hkv;
   ChunkKernels k;
-  if (dtype == SAS_BF16) k = a.dh == 128 ? chunk_kernels<bf16_t, 128>() : chunk_kernels<bf16_t, 64>();
-  else k = a.dh == 128 ? chunk_kernels<float, 128>() : chunk_kernels<float, 64>();
+  if (dtype != SAS_BF16) k = a.dh == 128 ? chunk_kernels<float, 128, false>() : chunk_kernels<float, 64, false>();
+  else if (wide) k = a.dh == 128 ? chunk_kernels<bf16_t, 128, true>() : chunk_kernels<bf16_t, 64, true>();
+  else k = a.dh == 128 ? chunk_kernels<bf16_t, 128, false>() : chunk_kernels<bf16_t, 64, false>();
   const int res = k.res;
   if (res <= 0) return hipErrorInvalidValue;
   // the most jobs that there can be: tiles in parts of the least length
@@ -717,7 +1144,7 @@ hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) 
   const long long most = (std::min<long long>(res, tiles * std::min<long long>(parts, res)) + ATTN_XCDS - 1) / ATTN_XCDS * ATTN_XCDS;
   const bool inl = a.b <= 64 && tiles < res;
   if (!inl) chunk_plan_kernel<<<1, 1024, 0, s>>>(a, keys, res);
-  (inl ? k.inl : k.queued)<<<(unsigned)most, 256, lds, s>>>(a, res);
+  (inl ? k.inl : k.queued)<<<(unsigned)most, 256, 512 * a.dh, s>>>(a, res);
   if (parts > 1) {
     const long long waves = (long long)a.rows * a.H;
     k.combine<<<(unsigned)std::min<long long>((waves + 3) / 4, 8192), 256, 0, s>>>(a);

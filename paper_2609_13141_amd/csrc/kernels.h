@@ -441,7 +441,9 @@ struct ChunkArgs {
   float* part_o;           // [part_rows, dh]
   float* part_ml;          // [part_rows, 2]
   long long part_rows;     // 0: no tile is divided
+  int tile_rows;           // rows of a tile (set by the launch)
 };
+constexpr int CHUNK_WIDE_ROWS = 128;  // of the kernel for long chunks
 // Rows of parts that a call works best with: twice the workgroups that the chip holds,
 // which is the most that parts of the average work of a workgroup can come to, of 128
 // rows.
