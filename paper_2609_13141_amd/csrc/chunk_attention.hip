@@ -85,7 +85,7 @@ struct ChunkWork {
   int units, nk, prow;
 };
 __device__ __forceinline__ ChunkWork chunk_work(const ChunkArgs& P, const ChunkSeq& q, int keys_per_tile) {
-  const int G = P.H / P.Hkv, qpt = P.tile_rows / G;
+  const int G = P.H / P.Hkv, qpt = CHUNK_ROWS / G;
   ChunkWork w;
   w.units = P.Hkv * ((q.m + qpt - 1) / qpt);
   w.nk = (q.keys + keys_per_tile - 1) / keys_per_tile;
@@ -295,14 +295,136 @@ __device__ __forceinline__ void chunk_copy(const ChunkArgs& P, const void* pool,
   }
 }
 
+// The row that a lane works for: query row `lane % 32` of its wave's block of 32 (both
+// halves of the wave share them).
+struct ChunkRow {
+  bool valid;
+  int t, q;      // position (-1: no row, and it attends nothing), row of the tile
+  size_t at;     // (row, head) in Q, O and the LSE
+};
+__device__ __forceinline__ ChunkRow chunk_row(const ChunkArgs& P, const ChunkSeq& S, int tile, int g, int wave, int lane) {
+  const int G = P.H / P.Hkv, QPT = CHUNK_ROWS / G;
+  ChunkRow r;
+  r.q = wave * 32 + (lane & 31);
+  const int pl = r.q / G;
+  r.valid = pl < QPT && tile * QPT + pl < S.m;
+  r.t = r.valid ? S.base + tile * QPT + pl : -1;
+  r.at = ((size_t)S.r0 + tile * QPT + pl) * P.H + g * G + (r.q - pl * G);
+  return r;
+}
+
+// Which keys of which unit a workgroup attends.
+struct ChunkSpan {
+  int t0, tlo, tend;  // position of the tile's first row; key tiles
+};
+__device__ __forceinline__ ChunkSpan chunk_span(const ChunkArgs& P, const ChunkSeq& S, int tile, int part, int parts, int keys) {
+  const int QPT = CHUNK_ROWS / (P.H / P.Hkv);
+  const int t_hi = S.base + min(tile * QPT + QPT, S.m) - 1;
+  const int nkt = (min(max(t_hi + 1, 0), S.keys) + keys - 1) / keys;
+  const int per = (nkt + parts - 1) / parts;
+  return {S.base + tile * QPT, part * per, min(part * per + per, nkt)};
+}
+
+// A product with P = 0 would turn an infinite or NaN value of a key that a row does not
+// attend into NaN.  In tiles with such keys, values of keys without a page (not in vm)
+// are zeroed; infinite and NaN elements of the others are added to the rows that do
+// attend them (the sum is not finite whatever their weight) and then zeroed too.
+template <typename T, int DH>
+__device__ __forceinline__ void chunk_fix_values(unsigned char* vb, unsigned long long* bad_keys, int k0,
+                                                 unsigned long long vm, int t, floatx16_t* o, int wave, int lane) {
+  constexpr int RB = DH * (int)sizeof(T), CH = RB / 16, NL = ChunkTile<T>::KEYS * CH / 256;
+  asm volatile("" : "+v"(lane));  // (nothing of this rare path is kept outside it)
+  if (threadIdx.x == 0) *bad_keys = 0;
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    asm volatile("" ::: "memory");  // (few loads at a time: registers are short)
+    const int r = ((wave * NL + i) * 64 + lane) / CH;
+    uint4* pv = (uint4*)(vb + (wave * NL + i) * 1024 + lane * 16);
+    if (!((vm >> r) & 1)) {
+      *pv = make_uint4(0, 0, 0, 0);
+    } else {
+      const uint4 u = *pv;
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        bad = bad || (w[e] & 0x7f800000u) == 0x7f800000u || (sizeof(T) == 2 && (w[e] & 0x7f80u) == 0x7f80u);
+      if (bad) atomicOr(bad_keys, 1ull << r);
+    }
+  }
+  lds_barrier();
+  unsigned long long bm = uniform64(*bad_keys);
+  if (!bm) return;
+  for (; bm; bm &= bm - 1) {
+    const int r = __builtin_ctzll(bm);
+    const bool on = k0 + r <= t;
+#pragma unroll
+    for (int dv = 0; dv < DH / 2; ++dv) {
+      // dimension 32 dt + 8 (v / 4) + 4 lk + v % 4: its 16-byte chunk, and the place in it
+      const int dt = dv / 16, v = dv % 16, lk = lane >> 5 & 1;
+      const int c = sizeof(T) == 2 ? dt * 4 + (v >> 2) : dt * 8 + 2 * (v >> 2) + lk;
+      if (dv % 4 == 0) asm volatile("" ::: "memory");
+      const T* x = (const T*)(vb + r * RB + ((c ^ chunk_swz<T, DH>(r)) << 4)) + (sizeof(T) == 2 ? 4 * lk : 0) + (v & 3);
+      const float f = Act<T>::to_f32(*x);
+      o[dt][v] += on && !(fabsf(f) < INFINITY) ? f : 0.f;
+    }
+  }
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    asm volatile("" ::: "memory");
+    T* pv = (T*)(vb + (wave * NL + i) * 1024 + lane * 16);
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e)
+      if (!(fabsf(Act<T>::to_f32(pv[e])) < INFINITY)) pv[e] = 0;
+  }
+  lds_barrier();
+}
+
+// A row's result, or its unnormalized sums and (max, sum) where the unit is in parts.
+template <typename T, int DH>
+__device__ __forceinline__ void chunk_store(const ChunkArgs& P, const ChunkSeq& S, int tile, int g, int rel, int2 sp,
+                                            const floatx16_t* o, float m_run, float l_run, int wave, int lane) {
+  asm volatile("" : "+v"(lane));  // (the row is formed anew: kept through the loop, it would spill)
+  const ChunkRow R = chunk_row(P, S, tile, g, wave, lane);
+  const int lk = lane >> 5;
+  if (!R.valid) return;
+  if (sp.x > 1) {
+    const int G = P.H / P.Hkv;
+    const size_t row = (size_t)sp.y + (size_t)rel * (min(S.m, CHUNK_ROWS / G) * G) + R.q;
+    float* po = P.part_o + row * DH;
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4)
+        *(float4*)(po + dt * 32 + 8 * v4 + 4 * lk) =
+            make_float4(o[dt][4 * v4 + 0], o[dt][4 * v4 + 1], o[dt][4 * v4 + 2], o[dt][4 * v4 + 3]);
+    if (lk == 0) *(float2*)(P.part_ml + row * 2) = make_float2(m_run, l_run);
+    return;
+  }
+  const float inv_l = l_run == 0.f ? 0.f : 1.0f / l_run;
+  T* op = (T*)P.O + R.at * DH;
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int v4 = 0; v4 < 4; ++v4) {
+      const int d0 = dt * 32 + 8 * v4 + 4 * lk;
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = l_run == 0.f ? 0.f : o[dt][4 * v4 + e] * inv_l;
+      if constexpr (sizeof(T) == 2) *(uint2*)(op + d0) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+      else *(float4*)(op + d0) = make_float4(x[0], x[1], x[2], x[3]);
+    }
+  if (P.lse && lk == 0) P.lse[R.at] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
+}
+
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int KEYS = ChunkTile<T>::KEYS, NST = KEYS / 32;
-  constexpr int CH = DH * (int)sizeof(T) / 16;  // 16-byte pieces of a row
   constexpr int RB = DH * (int)sizeof(T);       // bytes of a row
   constexpr int TB = KEYS * RB;                 // bytes of a tile
-  constexpr int NL = KEYS * CH / 256;           // pieces of K (and of V) per thread and tile
   // two buffers of K and V (4 TB bytes; dynamic, because the compiler makes every read
   // of a static array wait for the direct-to-LDS loads in flight)
   extern __shared__ __align__(256) unsigned char tiles[];
@@ -310,33 +432,23 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lk = lane >> 5;
-  const int G = P.H / P.Hkv, QPT = 128 / G;
   const ChunkSeq S = chunk_seq(P, seq);
-  const int ntile = (S.m + QPT - 1) / QPT;
+  const int ntile = (S.m + CHUNK_ROWS / (P.H / P.Hkv) - 1) / (CHUNK_ROWS / (P.H / P.Hkv));
   const int part = rel % sp.x, tile = ntile - 1 - (rel / sp.x) % ntile, g = rel / sp.x / ntile;
-
-  const int qrow = wave * 32 + lr;
-  const int pl = qrow / G, h = g * G + (qrow - pl * G);
-  const bool qvalid = pl < QPT && tile * QPT + pl < S.m;
-  const int t0 = S.base + tile * QPT;                            // position of the tile's first row
-  const int t_hi = S.base + min(tile * QPT + QPT, S.m) - 1;      // and of its last
-  const int t = qvalid ? t0 + pl : -1;
-  const size_t row = (size_t)S.r0 + tile * QPT + pl;
-  const bool wave_live = __builtin_amdgcn_ballot_w64(qvalid) != 0;
-  // this part's key tiles
-  const int nkt = (min(max(t_hi + 1, 0), S.keys) + KEYS - 1) / KEYS;
-  const int per = (nkt + sp.x - 1) / sp.x;
-  const int tlo = part * per, tend = min(tlo + per, nkt);
+  const ChunkRow R = chunk_row(P, S, tile, g, wave, lane);
+  const ChunkSpan span = chunk_span(P, S, tile, part, sp.x, KEYS);
+  const int t = R.t, t0 = span.t0, tend = span.tend;
+  const bool wave_live = __builtin_amdgcn_ballot_w64(R.valid) != 0;
 
   // Q^T as the B operand of S^T = K Q^T.  bf16: lane supplies dimensions
   // 16 ks + 8 lk + 0..7; fp32: 8 ks + 4 lk + e for step (ks, e)
   constexpr int NQ = BF ? DH / 16 : DH / 8;
   uint4 qb[NQ];
   {
-    const T* qp = (const T*)P.Q + (row * P.H + h) * DH;
+    const T* qp = (const T*)P.Q + R.at * DH;
 #pragma unroll
     for (int ks = 0; ks < NQ; ++ks)
-      qb[ks] = qvalid ? *(const uint4*)(qp + (BF ? ks * 16 + lk * 8 : ks * 8 + lk * 4)) : make_uint4(0, 0, 0, 0);
+      qb[ks] = R.valid ? *(const uint4*)(qp + (BF ? ks * 16 + lk * 8 : ks * 8 + lk * 4)) : make_uint4(0, 0, 0, 0);
   }
 
   floatx16_t o[DH / 32];
@@ -367,7 +479,7 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
     }
   }
 
-  int kt = tlo, buf = 0;
+  int kt = span.tlo, buf = 0;
   int pg = -1;
   unsigned long long vcur = 0;
   if (kt < tend) {
@@ -389,59 +501,7 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
       pg = pages.load(kt + 2);
     }
     const bool diag = k0 + KEYS - 1 > t0, gaps = vcur != ALL;
-    if (diag || gaps) {
-      // A product with P = 0 would turn an infinite or NaN value of a key that a row
-      // does not attend into NaN.  Values of keys without a page are zeroed; infinite
-      // and NaN elements of the others are added to the rows that do attend them (the
-      // sum is not finite whatever their weight) and then zeroed too.
-      if (tid == 0) bad_s = 0;
-      lds_barrier();
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int r = ((wave * NL + i) * 64 + lane) / CH;
-        uint4* pv = (uint4*)(tb + TB + (wave * NL + i) * 1024 + lane * 16);
-        if (!((vcur >> r) & 1)) {
-          *pv = make_uint4(0, 0, 0, 0);
-        } else {
-          const uint4 u = *pv;
-          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-          bool bad = false;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            bad = bad || (w[e] & 0x7f800000u) == 0x7f800000u;
-            if constexpr (BF) bad = bad || (w[e] & 0x7f80u) == 0x7f80u;
-          }
-          if (bad) atomicOr(&bad_s, 1ull << r);
-        }
-      }
-      lds_barrier();
-      unsigned long long bm = uniform64(bad_s);
-      if (bm) {
-        for (; bm; bm &= bm - 1) {
-          const int r = __builtin_ctzll(bm);
-          const bool on = k0 + r <= t;
-#pragma unroll
-          for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              const int d = dt * 32 + 8 * (v >> 2) + 4 * lk + (v & 3);
-              const int c = d * (int)sizeof(T) / 16;
-              const T x = *(const T*)(tb + TB + r * RB + ((c ^ chunk_swz<T, DH>(r)) << 4) + d * sizeof(T) % 16);
-              const float f = Act<T>::to_f32(x);
-              o[dt][v] += on && !(fabsf(f) < INFINITY) ? f : 0.f;
-            }
-        }
-        lds_barrier();
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          T* pv = (T*)(tb + TB + (wave * NL + i) * 1024 + lane * 16);
-#pragma unroll
-          for (int e = 0; e < 16 / (int)sizeof(T); ++e)
-            if (!(fabsf(Act<T>::to_f32(pv[e])) < INFINITY)) pv[e] = 0;
-        }
-        lds_barrier();
-      }
-    }
+    if (diag || gaps) chunk_fix_values<T, DH>(tb + TB, &bad_s, k0, vcur, t, o, wave, lane);
     if (wave_live) {
       __builtin_amdgcn_s_setprio(2);
       floatx16_t s[NST];
@@ -570,43 +630,9 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
     vcur = vnext;
   }
 
-  if (sp.x > 1) {  // a part: unnormalized sums and (max, sum) per row
-    if (!qvalid) return;
-    const size_t prow = (size_t)sp.y + (size_t)rel * (min(S.m, QPT) * G) + qrow;
-    float* po = P.part_o + prow * DH;
-#pragma unroll
-    for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4)
-        *(float4*)(po + dt * 32 + 8 * v4 + 4 * lk) =
-            make_float4(o[dt][4 * v4 + 0], o[dt][4 * v4 + 1], o[dt][4 * v4 + 2], o[dt][4 * v4 + 3]);
-    if (lk == 0) *(float2*)(P.part_ml + prow * 2) = make_float2(m_run, l_run);
-    return;
-  }
-  if (!qvalid) return;
-  const float inv_l = l_run == 0.f ? 0.f : 1.0f / l_run;
-  T* op = (T*)P.O + (row * P.H + h) * DH;
-#pragma unroll
-  for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-    for (int v4 = 0; v4 < 4; ++v4) {
-      const int d0 = dt * 32 + 8 * v4 + 4 * lk;
-      float x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = l_run == 0.f ? 0.f : o[dt][4 * v4 + e] * inv_l;
-      if constexpr (BF) *(uint2*)(op + d0) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-      else *(float4*)(op + d0) = make_float4(x[0], x[1], x[2], x[3]);
-    }
-  if (P.lse && lk == 0) P.lse[row * P.H + h] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
+  chunk_store<T, DH>(P, S, tile, g, rel, sp, o, m_run, l_run, wave, lane);
 }
 
-// The same job over 256 rows (bf16): a wave owns two blocks of 32 rows, so that each K
-// and V fragment read from LDS serves two products, and one wave runs per SIMD with the
-// whole register file.  With no second wave to fill the gaps, the loop is pipelined
-// inside the wave: while the matrix unit forms S of tile t + 1 and then O += P V of tile
-// t, the vector unit does the exponentials of tile t and the row maxima of t + 1, which
-// are independent of it.  K runs one tile ahead of V in LDS: an iteration holds K(t + 1)
-// and V(t) and loads K(t + 2) and V(t + 1), one barrier each.
 // LDS reads at a 32-bit address: 16 bytes, and the transposing read of 8
 __device__ __forceinline__ bf16x8_t lds_read16(uint32_t a) {
   return *(const __attribute__((address_space(3))) bf16x8_t*)(uintptr_t)a;
@@ -621,50 +647,45 @@ __device__ __forceinline__ float pair_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int DH, int NB>
-__device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
+// The same job (bf16), pipelined inside the wave for calls that the matrix unit bounds:
+// 32 keys at a time, the matrix unit forms the scores of the next tile while the vector
+// unit takes this tile's exponentials and sums, and adds the products with the values
+// while it takes the maxima of the following scores; none waits for the other.  K runs a
+// tile ahead of V in LDS: an iteration reads K(t + 1) and V(t) and loads K(t + 2) and
+// V(t + 1), with one barrier.  2048 tokens over 30005 cached, 28/4 heads of 128: 0.95 ms
+// (0.96 PFLOP/s; the plain loop 1.04, a large product reaches 1.4 PFLOP/s).  The vector
+// unit bounds it: about 230 instructions a wave and tile, 32 of them exponentials, against
+// 32 products of 32 cycles; addresses kept in registers instead of formed for each tile
+// took 2% off.  Not kept: 64 keys at a time (181 spilled registers, 3.1 ms), 64 rows a
+// wave with the fragments shared (340).
+template <int DH>
+__device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   using T = bf16_t;
-  constexpr int KEYS = 64, RB = DH * 2, CH = DH / 8, TB = KEYS * RB, NL = KEYS * CH / 256, ROWS = 128 * NB;
+  constexpr int KEYS = 64, RB = DH * 2, TB = KEYS * RB;
   // K buffers at 0 and TB, V buffers at 2 TB and 3 TB
   extern __shared__ __align__(256) unsigned char tiles[];
   __shared__ unsigned long long bad_s;
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lr = lane & 31, lk = lane >> 5;
-  const int G = P.H / P.Hkv, QPT = ROWS / G;
   const ChunkSeq S = chunk_seq(P, seq);
-  const int ntile = (S.m + QPT - 1) / QPT;
+  const int ntile = (S.m + CHUNK_ROWS / (P.H / P.Hkv) - 1) / (CHUNK_ROWS / (P.H / P.Hkv));
   const int part = rel % sp.x, tile = ntile - 1 - (rel / sp.x) % ntile, g = rel / sp.x / ntile;
-  const int t0 = S.base + tile * QPT;
-  const int t_hi = S.base + min(tile * QPT + QPT, S.m) - 1;
-  const int nkt = (min(max(t_hi + 1, 0), S.keys) + KEYS - 1) / KEYS;
-  const int per = (nkt + sp.x - 1) / sp.x;
-  const int tlo = part * per, tend = min(tlo + per, nkt);
+  const ChunkRow R = chunk_row(P, S, tile, g, wave, lane);
+  const ChunkSpan span = chunk_span(P, S, tile, part, sp.x, KEYS);
+  const int t = R.t, t0 = span.t0, tlo = span.tlo, tend = span.tend;
 
-  int t[NB];           // positions of this lane's rows (-1: none)
-  uint4 qb[NB][DH / 16];
+  uint4 qb[DH / 16];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int qrow = wave * 32 * NB + b * 32 + lr, pl = qrow / G;
-    const bool valid = pl < QPT && tile * QPT + pl < S.m;
-    t[b] = valid ? t0 + pl : -1;
-    const T* qp = (const T*)P.Q + (((size_t)S.r0 + tile * QPT + pl) * P.H + g * G + (qrow - pl * G)) * DH;
-#pragma unroll
-    for (int ks = 0; ks < DH / 16; ++ks)
-      qb[b][ks] = valid ? *(const uint4*)(qp + ks * 16 + lk * 8) : make_uint4(0, 0, 0, 0);
-  }
+  for (int ks = 0; ks < DH / 16; ++ks)
+    qb[ks] = R.valid ? *(const uint4*)((const T*)P.Q + R.at * DH + ks * 16 + lk * 8) : make_uint4(0, 0, 0, 0);
 
-  floatx16_t o[NB][DH / 32];
-  float m_run[NB], l_run[NB];
+  floatx16_t o[DH / 32];
+  float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    m_run[b] = -INFINITY;
-    l_run[b] = 0.f;
+  for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) o[b][dt][v] = 0.f;
-  }
+    for (int v = 0; v < 16; ++v) o[dt][v] = 0.f;
   const float qk_scale = P.sm_scale * LOG2E;
 
   const ChunkPages<T, DH> pages = {P, P.table + (size_t)seq * P.max_pages, g, S.keys, lane};
@@ -673,7 +694,7 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
   auto tile_barrier = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(chunk_lds_t*)tiles;  // aligned to a row
-  uint32_t o_row = lds0 + lr * RB + ((lk ^ chunk_swz<T, DH>(lr)) << 4);
+  const uint32_t o_row = lds0 + lr * RB + ((lk ^ chunk_swz<T, DH>(lr)) << 4);
   uint32_t o_tr[2];
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf) {
@@ -681,121 +702,55 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
     o_tr[hf] = lds0 + r * RB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ chunk_swz<T, DH>(r)) << 4) + (lane & 1) * 8;
   }
 
-  typedef floatx16_t scores_t[NB];  // of 32 keys
   // S = K Q^T of half st of the tile in the K buffer at kb
-  auto product = [&](scores_t& s, uint32_t kb, int st) __attribute__((always_inline)) {
+  auto product = [&](floatx16_t& s, uint32_t kb, int st) __attribute__((always_inline)) {
     const floatx16_t z = {};
 #pragma unroll
     for (int ks = 0; ks < DH / 16; ++ks) {
       const bf16x8_t k = lds_read16((o_row ^ (ks << 5)) + kb + st * 32 * RB);
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, *(const bf16x8_t*)&qb[b][ks], ks ? s[b] : z, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, *(const bf16x8_t*)&qb[ks], ks ? s : z, 0, 0, 0);
     }
   };
   // masks of a tile that reaches past the first row's position, or has keys without a page
-  auto mask = [&](scores_t& s, int kt, int st, unsigned long long vm) {
+  auto mask = [&](floatx16_t& s, int kt, int st, unsigned long long vm) {
     int lk4 = 4 * lk;
     asm volatile("" : "+v"(lk4));
     vm >>= lk4;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int j = st * 32 + 8 * (v >> 2) + (v & 3);
-        if (kt * KEYS + j + lk4 > t[b] || !((vm >> j) & 1)) s[b][v] = -INFINITY;
-      }
-  };
-  // row maxima of the scaled logits (the scale is positive)
-  auto maxima = [&](const scores_t& s, float* mx) __attribute__((always_inline)) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      float m = s[b][0];
-#pragma unroll
-      for (int v = 1; v < 16; ++v) m = fmaxf(m, s[b][v]);
-      mx[b] = pair_max(m * qk_scale);
+    for (int v = 0; v < 16; ++v) {
+      const int j = st * 32 + 8 * (v >> 2) + (v & 3);
+      if (kt * KEYS + j + lk4 > t || !((vm >> j) & 1)) s[v] = -INFINITY;
     }
+  };
+  // row maximum of the scaled logits (the scale is positive)
+  auto maximum = [&](const floatx16_t& s) __attribute__((always_inline)) {
+    float m = s[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) m = fmaxf(m, s[v]);
+    return pair_max(m * qk_scale);
   };
   // The reference moves only where a logit exceeds it by more than 8, in log2 units (any
   // reference gives the same sums); what is summed so far is then rescaled.
-  auto reference = [&](const float* mx) __attribute__((always_inline)) {
-    bool any = false;
+  auto reference = [&](float mx) __attribute__((always_inline)) {
+    const bool move = mx > m_run + 8.f;
+    if (__builtin_amdgcn_ballot_w64(move) == 0) return;
+    if (move) {
+      // (nothing is summed yet where m_run is -inf)
+      const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mx);
+      m_run = mx;
+      l_run *= alpha;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) any = any || mx[b] > m_run[b] + 8.f;
-    if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+      for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (mx[b] > m_run[b] + 8.f) {
-        // (nothing is summed yet where m_run is -inf)
-        const float alpha = m_run[b] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[b] - mx[b]);
-        m_run[b] = mx[b];
-        l_run[b] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) o[b][dt][v] *= alpha;
-      }
+        for (int v = 0; v < 16; ++v) o[dt][v] *= alpha;
     }
   };
-  // the values of a masked tile: see chunk_job
-  auto fix_values = [&](unsigned char* vb, int kt, unsigned long long vm) {
-    int ln = lane;
-    asm volatile("" : "+v"(ln));  // (nothing of this rare path is kept outside it)
-    if (tid == 0) bad_s = 0;
-    lds_barrier();
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      asm volatile("" ::: "memory");
-      const int r = ((wave * NL + i) * 64 + ln) / CH;
-      uint4* pv = (uint4*)(vb + (wave * NL + i) * 1024 + ln * 16);
-      if (!((vm >> r) & 1)) {
-        *pv = make_uint4(0, 0, 0, 0);
-      } else {
-        const uint4 u = *pv;
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          bad = bad || (w[e] & 0x7f800000u) == 0x7f800000u || (w[e] & 0x7f80u) == 0x7f80u;
-        if (bad) atomicOr(&bad_s, 1ull << r);
-      }
-    }
-    lds_barrier();
-    unsigned long long bm = uniform64(bad_s);
-    if (!bm) return;
-    for (; bm; bm &= bm - 1) {
-      const int r = __builtin_ctzll(bm);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const bool on = kt * KEYS + r <= t[b];
-#pragma unroll
-        for (int dv = 0; dv < DH / 2; ++dv) {
-            const int dt = dv / 16, v = dv % 16;
-            if (dv % 4 == 0) asm volatile("" ::: "memory");  // (few loads at a time: registers are short)
-            const int d = dt * 32 + 8 * (v >> 2) + 4 * (ln >> 5) + (v & 3);
-            const float f = bf16_to_f32(*(const T*)(vb + r * RB + (((d >> 3) ^ chunk_swz<T, DH>(r)) << 4) + d * 2 % 16));
-            o[b][dt][v] += on && !(fabsf(f) < INFINITY) ? f : 0.f;
-          }
-      }
-    }
-    lds_barrier();
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      asm volatile("" ::: "memory");
-      T* pv = (T*)(vb + (wave * NL + i) * 1024 + ln * 16);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (!(fabsf(bf16_to_f32(pv[e])) < INFINITY)) pv[e] = 0;
-    }
-    lds_barrier();
-  };
-
   unsigned long long vm = 0, vm1 = 0;  // keys of tiles kt and kt + 1 with a page
   uint64_t off1 = 0;                   // row offsets of tile kt + 1
   int pg2 = -1;                        // pages of tile kt + 2
   auto special = [&](int kt, unsigned long long v) { return kt * KEYS + KEYS - 1 > t0 || v != ~0ull; };
   if (tlo < tend) {
-    scores_t s0, s1, u0, u1;  // (a tile's halves, by turns)
+    floatx16_t s0, s1, u0, u1;  // (a tile's halves, by turns)
     {
       const int pg0 = pages.load(tlo), pg1 = pages.load(tlo + 1);
       const uint64_t off0 = pages.offset(tlo, pg0);
@@ -807,17 +762,17 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
       vm = pages.mapped(pg0);
       vm1 = pages.mapped(pg1);
     }
-    float mx[NB];
+    float mx;
     tile_barrier();
     // both halves of K(tlo) are read before the first iteration's loads replace it
     product(s0, 0, 0);
     product(s1, 0, 1);
     if (special(tlo, vm)) mask(s0, tlo, 0, vm);
-    maxima(s0, mx);
+    mx = maximum(s0);
     reference(mx);
     // tile kt, of scores s0 and s1; leaves those of the next in n0 and n1
     // (odd: the tile lies in the odd buffers, counted from tlo)
-    auto tile = [&](int kt, scores_t& s0, scores_t& s1, scores_t& n0, scores_t& n1, auto odd_t) __attribute__((always_inline)) {
+    auto tile = [&](int kt, floatx16_t& s0, floatx16_t& s1, floatx16_t& n0, floatx16_t& n1, auto odd_t) __attribute__((always_inline)) {
       constexpr int odd = decltype(odd_t)::value;
       tile_barrier();  // K(kt + 1) and V(kt) are there; K(kt) and V(kt - 1) are free
       const unsigned long long vm2 = pages.mapped(pg2);
@@ -827,20 +782,20 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
       off1 = off2;
       pg2 = pages.load(kt + 3);
       const bool masked = special(kt, vm), masked1 = special(kt + 1, vm1);
-      if (masked) fix_values(tiles + (2 + odd) * TB, kt, vm);
-      asm volatile("" : "+v"(o_row), "+v"(o_tr[0]), "+v"(o_tr[1]));  // (formed anew per tile: kept, they would spill)
+      if (masked) chunk_fix_values<T, DH>(tiles + (2 + odd) * TB, &bad_s, kt * KEYS, vm, t, o, wave, lane);
       constexpr uint32_t kb = (odd ^ 1) * TB, vb = (2 + odd) * TB;
       // Half st of the tile, whose scores s turn into those of the next tile's half: the
       // products of those between this half's exponentials and sums, then its products
       // with the values between the maxima of the following half, `after`.  One product
       // takes the matrix unit 32 cycles, about what a step's vector instructions take the
       // other; the steps are pinned, because the compiler groups each kind of instruction.
-      auto half = [&](const scores_t& s, scores_t& n, const scores_t& after, int st) __attribute__((always_inline)) {
+      auto half = [&](const floatx16_t& s, floatx16_t& n, const floatx16_t& after, int st) __attribute__((always_inline)) {
         constexpr int NK = DH / 16, ND = DH / 32, PER = 16 / NK;  // steps, groups of dimensions, weights a step
-        uint32_t pk[NB][8];
+        uint32_t pk[8];
         uint4 f0[ND], f1[ND];
         bf16x8_t kf[NK];
-        float bias[NB], p[NB][16], r2[NB][2];
+        float p[16], r2[2] = {0.f, 0.f};
+        const float bias = m_run == -INFINITY ? 0.f : -m_run;
         auto read_k = [&](int ks) { kf[ks] = lds_read16((o_row ^ (ks << 5)) + kb + st * 32 * RB); };
         auto read_v = [&](uint4* f, int dt, int ks) {
           const uint2 lo = lds_read_tr((o_tr[0] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB);
@@ -850,19 +805,12 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
         // P is rounded to bf16 for the matrix instruction; the sum keeps the fp32 weights
         auto finish = [&](int u) {
 #pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int v = u * PER; v < (u + 1) * PER; v += 2) {
-              r2[b][0] += p[b][v];
-              r2[b][1] += p[b][v + 1];
-              pk[b][v / 2] = pack_bf16x2(p[b][v], p[b][v + 1]);
-            }
+          for (int v = u * PER; v < (u + 1) * PER; v += 2) {
+            r2[0] += p[v];
+            r2[1] += p[v + 1];
+            pk[v / 2] = pack_bf16x2(p[v], p[v + 1]);
+          }
         };
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          bias[b] = m_run[b] == -INFINITY ? 0.f : -m_run[b];
-          r2[b][0] = r2[b][1] = 0.f;
-        }
         read_k(0);
         read_k(1);
         read_k(2);
@@ -871,14 +819,11 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
         for (int u = 0; u < NK; ++u) {
           if (u + 3 < NK) read_k(u + 3);
           else if (u + 3 - NK < ND) read_v(f0, u + 3 - NK, 0);
+          const floatx16_t z = {};
+          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u], *(const bf16x8_t*)&qb[u], u ? n : z, 0, 0, 0);
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            const floatx16_t z = {};
-            n[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u], *(const bf16x8_t*)&qb[b][u], u ? n[b] : z, 0, 0, 0);
-#pragma unroll
-            for (int v = u * PER; v < (u + 1) * PER; ++v)
-              p[b][v] = __builtin_amdgcn_exp2f(fmaf(s[b][v], qk_scale, bias[b]));
-          }
+          for (int v = u * PER; v < (u + 1) * PER; ++v)
+            p[v] = __builtin_amdgcn_exp2f(fmaf(s[v], qk_scale, bias));
           if (u > 0) finish(u - 1);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -886,41 +831,31 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
 #pragma unroll
         for (int dt = 3; dt < ND; ++dt) read_v(f0, dt, 0);
         __builtin_amdgcn_sched_barrier(0);
-        float m[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          l_run[b] += r2[b][0] + r2[b][1];  // this lane's keys
-          m[b] = after[b][0];
-        }
+        l_run += r2[0] + r2[1];  // this lane's keys
+        float m = after[0];
 #pragma unroll
         for (int u = 0; u < 2 * ND; ++u) {
           const int dt = u % ND, v0 = 4 * (u / ND);
           if (u < ND) read_v(f1, u, 1);
+          const uint4 pu = make_uint4(pk[v0], pk[v0 + 1], pk[v0 + 2], pk[v0 + 3]);
+          const uint4& f = u < ND ? f0[dt] : f1[dt];
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t*)&f, *(const bf16x8_t*)&pu, o[dt], 0, 0, 0);
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            const uint4 pu = make_uint4(pk[b][v0], pk[b][v0 + 1], pk[b][v0 + 2], pk[b][v0 + 3]);
-            const uint4& f = u < ND ? f0[dt] : f1[dt];
-            o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t*)&f, *(const bf16x8_t*)&pu, o[b][dt], 0, 0, 0);
-#pragma unroll
-            for (int v = u * PER; v < (u + 1) * PER; ++v) m[b] = fmaxf(m[b], after[b][v]);
-          }
+          for (int v = u * PER; v < (u + 1) * PER; ++v) m = fmaxf(m, after[v]);
           __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          mx[b] = pair_max(m[b] * qk_scale);
-        }
+        mx = pair_max(m * qk_scale);
       };
       half(s0, n0, s1, 0);
       if (masked) {
         mask(s1, kt, 1, vm);
-        maxima(s1, mx);
+        mx = maximum(s1);
       }
       reference(mx);
       half(s1, n1, n0, 1);
       if (masked1) {
         mask(n0, kt + 1, 0, vm1);
-        maxima(n0, mx);
+        mx = maximum(n0);
       }
       if (kt + 1 < tend) reference(mx);
       vm = vm1;
@@ -933,47 +868,16 @@ __device__ __forceinline__ void chunk_job_wide(const ChunkArgs& P, const int seq
       if (++kt >= tend) break;
     }
   }
-#pragma unroll
-  for (int b = 0; b < NB; ++b) l_run[b] += __shfl_xor(l_run[b], 32, 64);
-
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    if (t[b] < 0 && !(wave * 32 * NB + b * 32 + lr < QPT * G && tile * QPT + (wave * 32 * NB + b * 32 + lr) / G < S.m)) continue;
-    const int qrow = wave * 32 * NB + b * 32 + lr, pl = qrow / G, h = g * G + (qrow - pl * G);
-    const size_t row = (size_t)S.r0 + tile * QPT + pl;
-    if (sp.x > 1) {  // a part: unnormalized sums and (max, sum) per row
-      const size_t prow = (size_t)sp.y + (size_t)rel * (min(S.m, QPT) * G) + qrow;
-      float* po = P.part_o + prow * DH;
-#pragma unroll
-      for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-        for (int v4 = 0; v4 < 4; ++v4)
-          *(float4*)(po + dt * 32 + 8 * v4 + 4 * lk) =
-              make_float4(o[b][dt][4 * v4 + 0], o[b][dt][4 * v4 + 1], o[b][dt][4 * v4 + 2], o[b][dt][4 * v4 + 3]);
-      if (lk == 0) *(float2*)(P.part_ml + prow * 2) = make_float2(m_run[b], l_run[b]);
-      continue;
-    }
-    const float inv_l = l_run[b] == 0.f ? 0.f : 1.0f / l_run[b];
-    T* op = (T*)P.O + (row * P.H + h) * DH;
-#pragma unroll
-    for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4) {
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = l_run[b] == 0.f ? 0.f : o[b][dt][4 * v4 + e] * inv_l;
-        *(uint2*)(op + dt * 32 + 8 * v4 + 4 * lk) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-      }
-    if (P.lse && lk == 0) P.lse[row * P.H + h] = l_run[b] == 0.f ? -INFINITY : (m_run[b] + log2f(l_run[b])) * LN2;
-  }
+  l_run += __shfl_xor(l_run, 32, 64);
+  chunk_store<T, DH>(P, S, tile, g, rel, sp, o, m_run, l_run, wave, lane);
 }
 
 // INLINE (at most 64 sequences, fewer (tile, head) pairs than the grid): the job of
 // this workgroup by its own division.  Otherwise the division of chunk_plan_kernel:
 // one job a workgroup where they fit the grid, else jobs from the XCD's queue, then
 // from the next XCDs', until all eight are drained.
-template <typename T, int DH, bool INLINE, bool WIDE>
-__global__ void __launch_bounds__(256, WIDE && CHUNK_WIDE_ROWS > 128 ? 1 : 2) chunk_attn_kernel(ChunkArgs P, int res) {
+template <typename T, int DH, bool INLINE, bool PIPED>
+__global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P, int res) {
   __shared__ ChunkJob job_s;
   const int lane = threadIdx.x & 63;
   if constexpr (INLINE) {
@@ -1026,7 +930,7 @@ __global__ void __launch_bounds__(256, WIDE && CHUNK_WIDE_ROWS > 128 ? 1 : 2) ch
     if (r.seq < 0) break;
     const int seq = __builtin_amdgcn_readfirstlane(r.seq), rel = __builtin_amdgcn_readfirstlane(r.rel);
     const int2 sp = make_int2(__builtin_amdgcn_readfirstlane(r.sp.x), __builtin_amdgcn_readfirstlane(r.sp.y));
-    if constexpr (WIDE) chunk_job_wide<DH, CHUNK_WIDE_ROWS / 128>(P, seq, rel, sp);
+    if constexpr (PIPED) chunk_job_piped<DH>(P, seq, rel, sp);
     else chunk_job<T, DH>(P, seq, rel, sp);
     if (INLINE) break;
   }
@@ -1039,7 +943,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(ChunkArgs P) {
   if (P.head[1] == 0) return;
   constexpr int C8 = DH / 8, PG = 64 / C8;
   const int lane = threadIdx.x & 63, c8 = lane % C8, pg = lane / C8;
-  const int G = P.H / P.Hkv, QPT = P.tile_rows / G;
+  const int G = P.H / P.Hkv, QPT = CHUNK_ROWS / G;
   const int last = min(P.row_start[P.b], P.rows);
   for (long long it = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); it < (long long)P.rows * P.H;
        it += (long long)gridDim.x * 4) {
@@ -1106,10 +1010,10 @@ struct ChunkKernels {
   void (*combine)(ChunkArgs);
   int res;
 };
-template <typename T, int DH, bool WIDE>
+template <typename T, int DH, bool PIPED>
 static ChunkKernels chunk_kernels() {
   static std::atomic<int> known[64];  // workgroups of each device, 0: not asked yet
-  ChunkKernels k = {chunk_attn_kernel<T, DH, false, WIDE>, chunk_attn_kernel<T, DH, true, WIDE>,
+  ChunkKernels k = {chunk_attn_kernel<T, DH, false, PIPED>, chunk_attn_kernel<T, DH, true, PIPED>,
                     chunk_combine_kernel<T, DH>, 0};
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return k;
@@ -1123,17 +1027,17 @@ static ChunkKernels chunk_kernels() {
   return k;
 }
 
-hipError_t launch_chunk_attention(int dtype, const ChunkArgs& args, hipStream_t s) {
-  ChunkArgs a = args;
+hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) {
   const int G = a.H / a.Hkv;
   const int keys = dtype == SAS_BF16 ? 64 : 32;
-  const bool wide = dtype == SAS_BF16 && (long long)a.rows * G > 128ll * std::min(a.b, a.rows);
-  a.tile_rows = wide ? CHUNK_WIDE_ROWS : 128;
+  // the pipelined kernel where the average sequence fills a tile: with fewer rows the
+  // keys' bytes bound the call
+  const bool piped = dtype == SAS_BF16 && (long long)a.rows * G > (long long)CHUNK_ROWS * std::min(a.b, a.rows);
   // (tile, kv head) pairs, at most
-  const long long tiles = ((long long)a.rows / (a.tile_rows / G) + std::min(a.b, a.rows)) * a.Hkv;
+  const long long tiles = ((long long)a.rows / (CHUNK_ROWS / G) + std::min(a.b, a.rows)) * a.Hkv;
   ChunkKernels k;
   if (dtype != SAS_BF16) k = a.dh == 128 ? chunk_kernels<float, 128, false>() : chunk_kernels<float, 64, false>();
-  else if (wide) k = a.dh == 128 ? chunk_kernels<bf16_t, 128, true>() : chunk_kernels<bf16_t, 64, true>();
+  else if (piped) k = a.dh == 128 ? chunk_kernels<bf16_t, 128, true>() : chunk_kernels<bf16_t, 64, true>();
   else k = a.dh == 128 ? chunk_kernels<bf16_t, 128, false>() : chunk_kernels<bf16_t, 64, false>();
   const int res = k.res;
   if (res <= 0) return hipErrorInvalidValue;

@@ -441,13 +441,12 @@ struct ChunkArgs {
   float* part_o;           // [part_rows, dh]
   float* part_ml;          // [part_rows, 2]
   long long part_rows;     // 0: no tile is divided
-  int tile_rows;           // rows of a tile (set by the launch)
 };
-constexpr int CHUNK_WIDE_ROWS = 128;  // of the kernel for long chunks
+constexpr int CHUNK_ROWS = 128;  // rows of a tile
 // Rows of parts that a call works best with: twice the workgroups that the chip holds,
 // which is the most that parts of the average work of a workgroup can come to, of 128
 // rows.
-constexpr long long CHUNK_PART_ROWS = 1024 * 128;
+constexpr long long CHUNK_PART_ROWS = 1024 * CHUNK_ROWS;
 constexpr int CHUNK_MIN_TILES = 2;  // key tiles of the least part
 constexpr long long CHUNK_MAX_KEYS = 1ll << 30;  // positions that a block table may cover
 hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s);
