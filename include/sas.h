@@ -97,7 +97,8 @@ typedef enum {
   SAS_OP_SELECTION_STATS = 8,    /* sas_selection_stats: batch, seq_len */
   SAS_OP_QK_BACKWARD = 9,        /* sas_qk_norm_rope_backward: batch = rows, seq_len ignored */
   SAS_OP_ATTENTION_CHUNK = 10,   /* sas_attention_chunk: batch = sequences, seq_len = rows */
-  SAS_OP_VERIFY_DRAFTS = 11      /* sas_verify_drafts: batch = sequences, seq_len ignored (cfg is not read) */
+  SAS_OP_VERIFY_DRAFTS = 11,     /* sas_verify_drafts: batch = sequences, seq_len ignored (cfg is not read) */
+  SAS_OP_LAYER_CHUNK = 12        /* sas_layer_chunk: batch = sequences, seq_len = rows */
 } sas_op;
 
 typedef struct {
@@ -616,6 +617,26 @@ sas_status sas_cache_append(const sas_config* cfg, int32_t batch, int32_t rows, 
 sas_status sas_attention_chunk(const sas_config* cfg, int32_t batch, int32_t rows, const void* q,
                                const int32_t* row_start, const int32_t* kv_len, const sas_paged_kv* cache, void* o,
                                float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* A chunk's lengths and slots, as sas_plan_chunk gives them (DEVICE): row_start
+ * [b+1], ctx_len, kv_len [b] int32, slot [rows] int64. */
+typedef struct {
+  const int32_t* row_start;
+  const int32_t* ctx_len;
+  const int32_t* kv_len;
+  const int64_t* slot;
+} sas_chunk;
+
+/* One decoder layer over the chunk's rows x [rows, d] -> y [rows, d]:
+ * u1 = RMSNorm(x); Q, K, V = u1 W^T (rounded to the activation type), normed and
+ * rotated by rot and appended to the cache (sas_cache_append, w->w_gk projecting the
+ * summaries); attention over the cache (sas_attention_chunk); h1 = x + O W_o^T;
+ * y = h1 + SwiGLU(RMSNorm(h1)).  w->w_gq and w->decode_packed are not read.  Padding
+ * rows give unspecified outputs.  ws: sas_workspace_size(cfg, SAS_OP_LAYER_CHUNK,
+ * batch, rows); its last part, for partial sums, may be shorter or left out. */
+sas_status sas_layer_chunk(const sas_config* cfg, int32_t batch, int32_t rows, const void* x,
+                           const sas_layer_weights* w, const sas_rotary* rot, const sas_chunk* chunk,
+                           const sas_paged_kv* cache, void* y, void* ws, size_t ws_bytes, void* stream);
 
 /* Inputs of sas_verify_drafts, all DEVICE.  Sequence i drafted m = draft_start[i+1]
  * - draft_start[i] tokens (0 .. max_draft), `rows` in all.

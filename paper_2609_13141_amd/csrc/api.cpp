@@ -750,6 +750,34 @@ ChunkWs carve_chunk(Carve& cv, size_t total, const sas_config* c, int b) {
   return w;
 }
 
+struct LayerChunkWs {
+  void *u1, *q, *k, *v, *o, *h1;
+  float2* rope;
+  MlpWs mlp;
+  ChunkWs att;
+  size_t need;   // bytes up to here
+  float* part;   // what is left of the workspace: split products and, at another time, divided attention
+  size_t part_bytes;
+};
+LayerChunkWs carve_layer_chunk(Carve& cv, size_t total, const sas_config* c, int b, int rows) {
+  const size_t ab = act_bytes(c), T = rows, H = c->n_heads, Hkv = c->n_kv_heads, dh = c->head_dim;
+  LayerChunkWs w;
+  w.u1 = cv.take(T * c->d_model * ab);
+  w.rope = (float2*)cv.take(dh / 2 * sizeof(float2));
+  w.q = cv.take(T * H * dh * ab);
+  w.k = cv.take(T * Hkv * dh * ab);
+  w.v = cv.take(T * Hkv * dh * ab);
+  w.o = cv.take(T * H * dh * ab);
+  w.h1 = cv.take(T * c->d_model * ab);
+  w.mlp = carve_mlp(cv, c, T);
+  w.att = carve_chunk(cv, 0, c, b);
+  w.need = cv.off;
+  long long units = std::max(gemm_part_bytes(c, T, true), (size_t)CHUNK_PART_ROWS * chunk_part_bytes(c)) / 256;
+  w.part = (float*)cv.take_some(total, 256, units);
+  w.part_bytes = (size_t)units * 256;
+  return w;
+}
+
 sas_status check_chunk(int32_t batch, int32_t rows) {
   if (batch <= 0 || rows <= 0)
     return fail(SAS_ERR_INVALID_ARGUMENT, "batch %d and rows %d must be positive", batch, rows);
@@ -822,6 +850,85 @@ sas_status check_in_place(const void* in, long long stride, int heads, int dh, c
 }
 
 int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
+
+// `a` as qk_args filled it, over rows that are checked
+sas_status run_append(const sas_config* c, int batch, QkArgs a, const int64_t* slot, const int32_t* ctx_len,
+                      const int32_t* kv_len, const void* w_gk, const sas_paged_kv* cache, void* q_out, hipStream_t s) {
+  a.q_out = q_out;
+  a.slot = slot;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.num_pages = cache->num_pages;
+  a.ps_shift = shift_of(cache->page_size);
+  BlockSumArgs b = {};
+  b.b = batch;
+  b.rows = a.rows;
+  b.Hkv = a.Hkv;
+  b.dh = a.dh;
+  b.B = c->block_size;
+  b.ps_shift = a.ps_shift;
+  b.num_pages = cache->num_pages;
+  b.max_pages = cache->max_pages_per_seq;
+  b.max_blocks = cache->max_blocks;
+  b.ctx_len = ctx_len;
+  b.kv_len = kv_len;
+  b.table = cache->block_table;
+  b.k_pages = cache->k_pages;
+  b.w_gk = w_gk;
+  b.k_summary = cache->k_summary;
+  {
+    Timed tm("chunk_append", s);
+    HIP_TRY(launch_qk_norm_rope(c->dtype, a, s), "chunk append");
+  }
+  Timed tm("chunk_summaries", s);
+  HIP_TRY(launch_chunk_summaries(c->dtype, b, s), "chunk summaries");
+  return SAS_OK;
+}
+
+sas_status check_chunk_attention(const sas_config* c, int rows, const sas_paged_kv* cache) {
+  if (c->n_heads / c->n_kv_heads > 128)
+    return fail(SAS_ERR_UNSUPPORTED, "%d query heads per KV head (supported: <= 128)", c->n_heads / c->n_kv_heads);
+  if ((long long)cache->max_pages_per_seq * cache->page_size > CHUNK_MAX_KEYS)
+    return fail(SAS_ERR_UNSUPPORTED, "the block table covers %lld positions (supported: <= 2^30)",
+                (long long)cache->max_pages_per_seq * cache->page_size);
+  if ((long long)rows * c->n_heads > INT32_MAX / 2)
+    return fail(SAS_ERR_UNSUPPORTED, "%d rows of %d heads (supported: <= 2^30 heads)", rows, c->n_heads);
+  if ((unsigned long long)c->n_kv_heads * cache->page_size * c->head_dim * act_bytes(c) > 0xffffffffull)
+    return fail(SAS_ERR_UNSUPPORTED, "a page of %d KV heads has 4 GiB or more", c->n_kv_heads);
+  return SAS_OK;
+}
+
+sas_status run_chunk_attention(const sas_config* c, int batch, int rows, const void* q, const int32_t* row_start,
+                               const int32_t* kv_len, const sas_paged_kv* cache, void* o, float* lse, const ChunkWs& w,
+                               hipStream_t s) {
+  ChunkArgs a = {};
+  a.b = batch;
+  a.rows = rows;
+  a.H = c->n_heads;
+  a.Hkv = c->n_kv_heads;
+  a.dh = c->head_dim;
+  a.sm_scale = sm_scale_of(c);
+  a.Q = q;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.table = cache->block_table;
+  a.num_pages = cache->num_pages;
+  a.ps_shift = shift_of(cache->page_size);
+  a.max_pages = cache->max_pages_per_seq;
+  a.row_start = row_start;
+  a.kv_len = kv_len;
+  a.O = o;
+  a.lse = lse;
+  a.head = w.head;
+  a.job_base = w.job_base;
+  a.seq_parts = w.seq_parts;
+  a.part_rows = w.part_rows;
+  a.part_o = w.part;
+  a.part_ml = w.part ? w.part + (size_t)w.part_rows * c->head_dim : nullptr;
+  Timed tm("attention_chunk", s);
+  HIP_TRY(launch_chunk_attention(c->dtype, a, s), "chunk attention");
+  return SAS_OK;
+}
 
 }  // namespace
 
@@ -918,6 +1025,10 @@ size_t sas_workspace_size(const sas_config* c, int32_t op, int32_t batch, int32_
       break;
     case SAS_OP_VERIFY_DRAFTS:
       cv.take(verify_part_bytes(batch));
+      break;
+    case SAS_OP_LAYER_CHUNK:
+      if (seq_len <= 0 || batch > CHUNK_MAX_SEQS || check_config(c, true) != SAS_OK) return 0;
+      carve_layer_chunk(cv, SIZE_MAX, c, batch, seq_len);
       break;
     default:
       return 0;
@@ -1750,36 +1861,7 @@ sas_status sas_cache_append(const sas_config* c, int32_t batch, int32_t rows, co
   SAS_TRY(check_in_place(in->q, a.qs, a.H, a.dh, q_out, "q_out"));
   if (!cache) return fail(SAS_ERR_INVALID_ARGUMENT, "cache is NULL");
   SAS_TRY(check_cache(c, cache));
-  a.q_out = q_out;
-  a.slot = slot;
-  a.k_pages = cache->k_pages;
-  a.v_pages = cache->v_pages;
-  a.num_pages = cache->num_pages;
-  a.ps_shift = shift_of(cache->page_size);
-  BlockSumArgs b = {};
-  b.b = batch;
-  b.rows = rows;
-  b.Hkv = a.Hkv;
-  b.dh = a.dh;
-  b.B = c->block_size;
-  b.ps_shift = a.ps_shift;
-  b.num_pages = cache->num_pages;
-  b.max_pages = cache->max_pages_per_seq;
-  b.max_blocks = cache->max_blocks;
-  b.ctx_len = ctx_len;
-  b.kv_len = kv_len;
-  b.table = cache->block_table;
-  b.k_pages = cache->k_pages;
-  b.w_gk = w_gk;
-  b.k_summary = cache->k_summary;
-  hipStream_t s = (hipStream_t)stream;
-  {
-    Timed tm("chunk_append", s);
-    HIP_TRY(launch_qk_norm_rope(c->dtype, a, s), "chunk append");
-  }
-  Timed tm("chunk_summaries", s);
-  HIP_TRY(launch_chunk_summaries(c->dtype, b, s), "chunk summaries");
-  return SAS_OK;
+  return run_append(c, batch, a, slot, ctx_len, kv_len, w_gk, cache, q_out, (hipStream_t)stream);
 }
 
 sas_status sas_attention_chunk(const sas_config* c, int32_t batch, int32_t rows, const void* q,
@@ -1794,46 +1876,85 @@ sas_status sas_attention_chunk(const sas_config* c, int32_t batch, int32_t rows,
   SAS_TRY(check_ptr(lse, "lse", false));
   if (!cache) return fail(SAS_ERR_INVALID_ARGUMENT, "cache is NULL");
   SAS_TRY(check_cache(c, cache));
-  if (c->n_heads / c->n_kv_heads > 128)
-    return fail(SAS_ERR_UNSUPPORTED, "%d query heads per KV head (supported: <= 128)", c->n_heads / c->n_kv_heads);
-  if ((long long)cache->max_pages_per_seq * cache->page_size > CHUNK_MAX_KEYS)
-    return fail(SAS_ERR_UNSUPPORTED, "the block table covers %lld positions (supported: <= 2^30)",
-                (long long)cache->max_pages_per_seq * cache->page_size);
-  if ((long long)rows * c->n_heads > INT32_MAX / 2)
-    return fail(SAS_ERR_UNSUPPORTED, "%d rows of %d heads (supported: <= 2^30 heads)", rows, c->n_heads);
-  if ((unsigned long long)c->n_kv_heads * cache->page_size * c->head_dim * act_bytes(c) > 0xffffffffull)
-    return fail(SAS_ERR_UNSUPPORTED, "a page of %d KV heads has 4 GiB or more", c->n_kv_heads);
+  SAS_TRY(check_chunk_attention(c, rows, cache));
   Carve cv(ws);
   const ChunkWs w = carve_chunk(cv, ws_bytes, c, batch);
   SAS_TRY(check_ws(ws, ws_bytes, w.need));
-  ChunkArgs a = {};
-  a.b = batch;
-  a.rows = rows;
-  a.H = c->n_heads;
-  a.Hkv = c->n_kv_heads;
-  a.dh = c->head_dim;
-  a.sm_scale = sm_scale_of(c);
-  a.Q = q;
-  a.k_pages = cache->k_pages;
-  a.v_pages = cache->v_pages;
-  a.table = cache->block_table;
-  a.num_pages = cache->num_pages;
-  a.ps_shift = shift_of(cache->page_size);
-  a.max_pages = cache->max_pages_per_seq;
-  a.row_start = row_start;
-  a.kv_len = kv_len;
-  a.O = o;
-  a.lse = lse;
-  a.head = w.head;
-  a.job_base = w.job_base;
-  a.seq_parts = w.seq_parts;
-  a.part_rows = w.part_rows;
-  a.part_o = w.part;
-  a.part_ml = w.part ? w.part + (size_t)w.part_rows * c->head_dim : nullptr;
+  return run_chunk_attention(c, batch, rows, q, row_start, kv_len, cache, o, lse, w, (hipStream_t)stream);
+}
+
+sas_status sas_layer_chunk(const sas_config* c, int32_t batch, int32_t rows, const void* x, const sas_layer_weights* w,
+                           const sas_rotary* rot, const sas_chunk* chunk, const sas_paged_kv* cache, void* y, void* ws,
+                           size_t ws_bytes, void* stream) {
+  SAS_TRY(check_config(c, true));
+  SAS_TRY(check_chunk(batch, rows));
+  SAS_TRY(check_ptr(x, "x", true));
+  SAS_TRY(check_ptr(y, "y", true));
+  SAS_TRY(check_weights(w, true, true));
+  if (!chunk || !cache) return fail(SAS_ERR_INVALID_ARGUMENT, "chunk/cache is NULL");
+  SAS_TRY(check_ptr(chunk->row_start, "chunk.row_start", true));
+  SAS_TRY(check_ptr(chunk->ctx_len, "chunk.ctx_len", true));
+  SAS_TRY(check_ptr(chunk->kv_len, "chunk.kv_len", true));
+  SAS_TRY(check_ptr(chunk->slot, "chunk.slot", true));
+  SAS_TRY(check_cache(c, cache));
+  SAS_TRY(check_chunk_attention(c, rows, cache));
+  Carve cv(ws);
+  LayerChunkWs lw = carve_layer_chunk(cv, ws_bytes, c, batch, rows);
+  SAS_TRY(check_ws(ws, ws_bytes, lw.need));
+  const sas_qkv qkv = {lw.q, lw.k, lw.v, 0, 0, 0};
+  QkArgs qa;
+  SAS_TRY(qk_args(c, rows, rot, &qkv, true, qa));
   hipStream_t s = (hipStream_t)stream;
-  Timed tm("attention_chunk", s);
-  HIP_TRY(launch_chunk_attention(c->dtype, a, s), "chunk attention");
-  return SAS_OK;
+  {
+    // the rotary table's row of position 0 alone: the product's epilogue rotates by nothing
+    Timed tm("rmsnorm", s);
+    HIP_TRY(launch_rmsnorm_rope(c->dtype, x, w->rms1, lw.u1, rows, c->d_model, c->rms_eps, nullptr, lw.rope, c->head_dim,
+                                c->rope_base, 1, s),
+            "rmsnorm");
+  }
+  GemmArgs g = {};
+  g.epi = EPI_QKV_ROPE;
+  g.M = rows;
+  g.K = c->d_model;
+  g.A = lw.u1;
+  g.B0 = w->wq;
+  g.B1 = w->wk;
+  g.B2 = w->wv;
+  g.N = (c->n_heads + 2 * c->n_kv_heads) * c->head_dim;
+  g.out = lw.q;
+  g.out1 = lw.k;
+  g.out2 = lw.v;
+  g.n_heads = c->n_heads;
+  g.n_kv_heads = c->n_kv_heads;
+  g.head_dim = c->head_dim;
+  g.seq_len = 1;
+  g.rope = lw.rope;
+  g.part = lw.part;
+  g.part_bytes = lw.part_bytes;
+  {
+    Timed tm("gemm_qkv", s);
+    HIP_TRY(linear(c->dtype, g, s), "qkv gemm");
+  }
+  SAS_TRY(run_append(c, batch, qa, chunk->slot, chunk->ctx_len, chunk->kv_len, w->w_gk, cache, lw.q, s));
+  lw.att.part = lw.part;
+  lw.att.part_rows = std::min<long long>(CHUNK_PART_ROWS, lw.part_bytes / chunk_part_bytes(c));
+  SAS_TRY(run_chunk_attention(c, batch, rows, lw.q, chunk->row_start, chunk->kv_len, cache, lw.o, nullptr, lw.att, s));
+  GemmArgs og = {};
+  og.epi = EPI_RESID;
+  og.M = rows;
+  og.K = c->n_heads * c->head_dim;
+  og.A = lw.o;
+  og.B0 = w->wo;
+  og.N = c->d_model;
+  og.resid = x;
+  og.out = lw.h1;
+  og.part = lw.part;
+  og.part_bytes = lw.part_bytes;
+  {
+    Timed tm("gemm_o", s);
+    HIP_TRY(linear(c->dtype, og, s), "o-proj gemm");
+  }
+  return run_mlp(c, (size_t)rows, lw.h1, w, y, lw.mlp, GemmPart{lw.part, lw.part_bytes}, s);
 }
 
 sas_status sas_verify_drafts(int32_t batch, int32_t rows, int32_t vocab, int32_t max_draft, const sas_verify_in* in,

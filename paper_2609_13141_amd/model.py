@@ -5,6 +5,8 @@ layer's paged KV cache and block summaries; every generated token is then
 embedded, runs the SAS decode step in each layer (Top-K blocks per KV group
 by the selector, attention to them plus the current block without gate bias)
 and the greedy LM head (final RMSNorm, logits in fp32, lowest id on ties).
+Sequences may also take several new tokens at once over what is cached (a piece
+of a long prompt, drafted tokens): ``extend``, a dense chunk in every layer.
 Every step runs in the library's kernels; this module only sequences them.
 """
 from __future__ import annotations
@@ -79,6 +81,27 @@ class Stack:
         self.pos += 1
         out = (nxt, lg, (sels if sel_idx else None))
         return out + (tps,) if taps else out
+
+    def extend(self, ids, ctx_len, new_len):
+        """New tokens of every sequence, any number each, over the caches: ids
+        [rows] int32, sequence i's new_len[i] after each other at positions
+        ctx_len[i] .. (ctx_len, new_len [b] int32, all on the device; rows past
+        their sum are padding).  Returns the last layer's output [rows, d] and
+        the rows' plan (see sas.plan_chunk)."""
+        x = sas.embed(self.cfg_prefill, ids.view(1, -1), self.ends["embed"])[0]
+        none = torch.zeros(1, dtype=torch.int32, device=ids.device)
+        plan = None
+        for W, cache in zip(self.layers, self.caches):
+            # (every position's page is there already, in another order in each layer)
+            held = torch.full_like(ctx_len, cache.block_table.shape[1])
+            plan = sas.plan_chunk(cache, ctx_len, new_len, held, none, none, ids.numel())
+            x = sas.layer_chunk(self.cfg_prefill, x, W, cache, ctx_len, plan, ws=self.ws)
+        return x, plan
+
+    def logits(self, x):
+        """fp32 logits [rows, V] of hidden rows x [rows, d], 16 at a time (the LM head's rows)."""
+        return torch.cat([sas.lm_head_argmax(self.cfg_decode, r.contiguous(), self.ends["rms_final"], self.ends["w_lm"],
+                                             logits=True, ws=self.ws)[1] for r in x.split(16)])
 
     def generate(self, ids, img, steps: int):
         """Greedy generation: [b, steps + 1] tokens (the prefill's and `steps` more)."""

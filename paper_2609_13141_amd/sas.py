@@ -24,14 +24,15 @@ GATE_POS = {"inner": 0, "outer": 1}
 GATE_ACT = {"softmax": 0, "sigmoid": 1, "raw": 2}
 SCOPES = {"sparse": 0, "full": 1}
 (OP_ATTENTION, OP_MLP, OP_LAYER, OP_DECODE, OP_LM_HEAD, OP_DECODE_SELECT, OP_ATTENTION_BACKWARD,
- OP_SELECTOR_BACKWARD, OP_SELECTION_STATS, OP_QK_BACKWARD, OP_ATTENTION_CHUNK, OP_VERIFY_DRAFTS) = range(12)
+ OP_SELECTOR_BACKWARD, OP_SELECTION_STATS, OP_QK_BACKWARD, OP_ATTENTION_CHUNK, OP_VERIFY_DRAFTS,
+ OP_LAYER_CHUNK) = range(13)
 TORCH_DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 EXPORTS = ("sas_workspace_size", "sas_attention_prefill", "sas_mlp_forward", "sas_layer_forward",
            "sas_decode_step", "sas_decode_step_noalloc", "sas_decode_select", "sas_attention_backward", "sas_selector_backward", "sas_selection_stats", "sas_overlap_recall", "sas_embed", "sas_lm_head_argmax", "sas_last_error", "sas_version",
            "sas_profiler_start", "sas_profiler_select", "sas_profiler_stop", "sas_profiler_record",
            "sas_decode_packed_bytes", "sas_pack_decode_weights", "sas_plan_chunk", "sas_qk_norm_rope",
-           "sas_qk_norm_rope_backward", "sas_cache_append", "sas_attention_chunk", "sas_verify_drafts")
+           "sas_qk_norm_rope_backward", "sas_cache_append", "sas_attention_chunk", "sas_verify_drafts", "sas_layer_chunk")
 
 
 class SasError(RuntimeError):
@@ -118,6 +119,10 @@ class Qkv(C.Structure):
                 ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
 
 
+class Chunk(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("row_start", "ctx_len", "kv_len", "slot")]
+
+
 class VerifyIn(C.Structure):
     _fields_ = [(f, C.c_void_p) for f in ("target", "draft", "tokens", "draft_start", "u_accept", "u_sample")]
 
@@ -195,6 +200,9 @@ def lib() -> C.CDLL:
                                    C.POINTER(PagedKV), vp, vp]
     L.sas_attention_chunk.restype = i32
     L.sas_attention_chunk.argtypes = [C.POINTER(Config), i32, i32, vp, vp, vp, C.POINTER(PagedKV), vp, vp, vp, sz, vp]
+    L.sas_layer_chunk.restype = i32
+    L.sas_layer_chunk.argtypes = [C.POINTER(Config), i32, i32, vp, C.POINTER(LayerWeights), C.POINTER(Rotary),
+                                  C.POINTER(Chunk), C.POINTER(PagedKV), vp, vp, sz, vp]
     L.sas_verify_drafts.restype = i32
     L.sas_verify_drafts.argtypes = [i32, i32, i32, i32, C.POINTER(VerifyIn), vp, vp, vp, sz, vp]
     _lib = L
@@ -759,6 +767,28 @@ def attention_chunk(cfg: Config, q, cache: PagedCache, row_start, kv_len, *, lse
         _call(dev, lib().sas_attention_chunk, C.byref(cfg), b, rows, qp, rp, kl, C.byref(kv), op,
               r["lse"].data_ptr() if lse else None, buf.data_ptr(), buf.numel())
     return r
+
+
+def layer_chunk(cfg: Config, x, W: dict, cache: PagedCache, ctx_len, plan: dict, pos=None, gain_q=None, gain_k=None, *,
+                sections=None, ws: Workspace | None = None):
+    """One decoder layer over a chunk's rows x [rows, d]: plan is plan_chunk's (for
+    this cache) of ctx_len [b]; pos [axes, rows] int32 are the rotary positions (None:
+    the plan's).  Appends the chunk to the cache; returns y [rows, d]."""
+    dev = _device("x", x)
+    rows, b = x.shape[0], ctx_len.numel()
+    i32 = torch.int32
+    xp = _need("x", x, _act(cfg), (rows, cfg.d_model), dev)
+    y = torch.empty_like(x)
+    if not rows:
+        return y
+    rot = _rotary(cfg, plan["pos"] if pos is None else pos, gain_q, gain_k, sections, rows, dev)
+    ch = Chunk(_need("row_start", plan["row_start"], i32, (b + 1,), dev), _need("ctx_len", ctx_len, i32, (b,), dev),
+               _need("kv_len", plan["kv_len"], i32, (b,), dev), _need("slot", plan["slot"], torch.int64, (rows,), dev))
+    kv = _cache_arg(cfg, cache, b, dev)
+    buf = _scratch(ws, workspace_size(cfg, OP_LAYER_CHUNK, b, rows), dev)
+    _call(dev, lib().sas_layer_chunk, C.byref(cfg), b, rows, xp, C.byref(weights_struct(W)), C.byref(rot), C.byref(ch),
+          C.byref(kv), y.data_ptr(), buf.data_ptr(), buf.numel())
+    return y
 
 
 def verify_drafts(target, draft, tokens, draft_start, u_accept, u_sample, max_draft: int, *,

@@ -145,6 +145,24 @@ def test_verify(L):
     assert sas.lib().sas_workspace_size(None, sas.OP_ATTENTION_CHUNK, 3, 4) == 0
 
 
+def test_layer(L):
+    cfg = config(4, 2, 128)
+    W = sas.LayerWeights(*([P] * 9 + [None, None, None]))
+    ch = dict(row_start=P, ctx_len=P, kv_len=P, slot=P)
+
+    def call(cfg=cfg, b=2, rows=4, x=P, W=W, rot=rotary(), cache=kv(), y=0x2000, ws=P, n=1 << 30, **kw):
+        c = sas.Chunk(*[{**ch, **kw}[f] for f, _ in sas.Chunk._fields_])
+        return L.sas_layer_chunk(C.byref(cfg), b, rows, x, C.byref(W), C.byref(rot) if rot else None, C.byref(c),
+                                 C.byref(cache) if cache else None, y, ws, n, None)
+    assert call(b=0) == BAD and call(rows=0) == BAD and call(b=5000) == UNSUP
+    for k in ("x", "y", "cache", "row_start", "ctx_len", "kv_len", "slot", "rot"):
+        assert call(**{k: None}) == BAD, k
+    assert call(W=sas.LayerWeights()) == BAD and b"w.rms1" in L.sas_last_error()
+    assert call(rot=rotary(section=(3, 0, 0))) == BAD and call(cache=kv(page_size=48)) == BAD
+    assert call(ws=None) == WS and call(n=4096) == WS
+    assert sas.workspace_size(cfg, sas.OP_LAYER_CHUNK, 2, 0) == 0
+
+
 def test_the_binding_refuses_host_tensors():
     t = torch.zeros(4, 4, 128, dtype=torch.bfloat16)
     i = torch.zeros(4, dtype=torch.int32)
