@@ -591,8 +591,8 @@ def _refuse(name: str, what: str, t):
 
 def _need(name: str, t, dtype, shape: tuple, dev) -> int:
     """The address of t, a contiguous tensor of that type and shape (-1: any size) on `dev`."""
-    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == dev and t.is_contiguous():
-        got = tuple(t.shape)
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == dev and t.is_contiguous():
+        got = t.shape
         if got == shape or (len(got) == len(shape) and all(w in (-1, n) for n, w in zip(got, shape))):
             return t.data_ptr()
     _refuse(name, f"contiguous {dtype} {list(shape)} on {dev}", t)
@@ -606,11 +606,14 @@ def _device(name: str, t):
 
 def _call(dev, fn, *args):
     """fn(*args, current stream of dev), with dev the current device."""
-    if torch.cuda.current_device() == dev.index:
-        _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev.index)))
+    i = dev.index
+    if torch._C._cuda_getDevice() == i:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev.index)))
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    if status != SAS_OK:
+        _check(status)
 
 
 def _act(cfg: Config):
@@ -627,10 +630,10 @@ def _scratch(ws: Workspace | None, nbytes: int, dev):
 def _cache_arg(cfg: Config, cache: PagedCache, b: int, dev) -> PagedKV:
     Hkv, dh, act, ps = cfg.n_kv_heads, cfg.head_dim, _act(cfg), cache.page_size
     k, v, t, s = cache.k_pages, cache.v_pages, cache.block_table, cache.k_summary
-    return PagedKV(_need("cache.k_pages", k, act, (-1, Hkv, ps, dh), dev),
-                   _need("cache.v_pages", v, act, tuple(k.shape), dev),
-                   _need("cache.block_table", t, torch.int32, (b, -1), dev),
-                   _need("cache.k_summary", s, act, (b, Hkv, -1, dh), dev), k.shape[0], ps, t.shape[1], s.shape[2])
+    pages = (k.shape[0], Hkv, ps, dh)
+    return PagedKV(_need("cache.k_pages", k, act, pages, dev), _need("cache.v_pages", v, act, pages, dev),
+                   _need("cache.block_table", t, torch.int32, (b, t.shape[-1]), dev),
+                   _need("cache.k_summary", s, act, (b, Hkv, s.shape[-2], dh), dev), pages[0], ps, t.shape[1], s.shape[2])
 
 
 def _heads_arg(cfg: Config, name: str, t, heads: int, rows: int, dev):
@@ -665,21 +668,25 @@ def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free
     b = ctx_len.numel()
     i32 = torch.int32
     table = cache.block_table
-    kv = PagedKV(None, None, _need("cache.block_table", table, i32, (b, -1), dev), None, cache.k_pages.shape[0],
+    kv = PagedKV(None, None, _need("cache.block_table", table, i32, (b, table.shape[-1]), dev), None, cache.k_pages.shape[0],
                  cache.page_size, table.shape[1], 0)
     pi = PlanIn(_need("ctx_len", ctx_len, i32, (b,), dev), _need("new_len", new_len, i32, (b,), dev),
-                _need("pages_held", pages_held, i32, (b,), dev), _need("free_pages", free_pages, i32, (-1,), dev),
+                _need("pages_held", pages_held, i32, (b,), dev), _need("free_pages", free_pages, i32, (free_pages.numel(),), dev),
                 _need("free_count", free_count, i32, (1,), dev), free_pages.numel())
     if rows <= 0:
         raise SasError(SAS_ERR_INVALID_ARGUMENT, f"rows {rows} must be positive")
-    # one allocation: 16-byte aligned pieces, the gaps dropped
-    gap = lambda n: -n % 4  # noqa: E731
-    row_start, _, kv_len, _, held, _, seq, _, pos, _, free, _, missing, _ = torch.empty(
-        2 * (rows + gap(rows)) + 2 * (b + gap(b)) + b + 1 + gap(b + 1) + 8, dtype=i32, device=dev).split(
-        [b + 1, gap(b + 1), b, gap(b), b, gap(b), rows, gap(rows), rows, gap(rows), 1, 3, 1, 3])
-    out = {"row_start": row_start, "kv_len": kv_len, "seq": seq, "pos": pos,
-           "slot": torch.empty(rows, dtype=torch.int64, device=dev), "pages_held": held, "free_count": free,
-           "missing": missing}
+    # one allocation for the int32 outputs, each at a multiple of 16 bytes
+    sizes, names = [], []
+    for name, n in (("seq", rows), ("pos", rows), ("kv_len", b), ("pages_held", b), ("row_start", b + 1),
+                    ("free_count", 1), ("missing", 1)):
+        sizes.append(n)
+        names.append(name)
+        if n % 4:
+            sizes.append(-n % 4)
+            names.append(None)
+    out = dict(zip(names, torch.empty(sum(sizes), dtype=i32, device=dev).split_with_sizes(sizes)))
+    out.pop(None, None)
+    out["slot"] = torch.empty(rows, dtype=torch.int64, device=dev)
     po = PlanOut(*[out[f].data_ptr() for f, _ in PlanOut._fields_])
     _call(dev, lib().sas_plan_chunk, b, rows, C.byref(pi), C.byref(kv), C.byref(po))
     return out
@@ -803,8 +810,8 @@ def verify_drafts(target, draft, tokens, draft_start, u_accept, u_sample, max_dr
     f32, i32 = torch.float32, torch.int32
     if max_draft < 0:
         raise SasError(SAS_ERR_INVALID_ARGUMENT, f"max_draft {max_draft} is negative")
-    tp = _need("target", target, f32, (rows + b, -1), dev)
-    V = target.shape[1]
+    V = target.shape[-1]
+    tp = _need("target", target, f32, (rows + b, V), dev)
     dp = None if draft is None else _need("draft", draft, f32, (rows, V), dev)
     vi = VerifyIn(tp, dp or None, _need("tokens", tokens, i32, (rows,), dev),
                   _need("draft_start", draft_start, i32, (b + 1,), dev), _need("u_accept", u_accept, f32, (rows,), dev),
