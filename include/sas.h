@@ -97,8 +97,8 @@ typedef enum {
   SAS_OP_SELECTION_STATS = 8,    /* sas_selection_stats: batch, seq_len */
   SAS_OP_QK_BACKWARD = 9,        /* sas_qk_norm_rope_backward: batch = rows, seq_len ignored */
   SAS_OP_ATTENTION_CHUNK = 10,   /* sas_attention_chunk: batch = sequences, seq_len = rows */
-  SAS_OP_VERIFY_DRAFTS = 11,     /* sas_verify_drafts: batch = sequences, seq_len ignored (cfg is not read) */
-  SAS_OP_LAYER_CHUNK = 12        /* sas_layer_chunk: batch = sequences, seq_len = rows */
+  SAS_OP_LAYER_CHUNK = 11,       /* sas_layer_chunk: batch = sequences, seq_len = rows */
+  SAS_OP_VERIFY_DRAFTS = 12      /* sas_verify_drafts: batch = sequences, seq_len = vocab (cfg is not read) */
 } sas_op;
 
 typedef struct {
@@ -665,7 +665,8 @@ typedef struct {
  * does; -1 if all weights are zero).  Products, differences and sums are fp64; weights that are negative
  * or NaN count as zero.
  * out_tokens [b, max_draft + 1] int32: the accepted tokens, the drawn one, -1;
- * accepted [b] int32.  ws: sas_workspace_size(NULL, SAS_OP_VERIFY_DRAFTS, batch, 0). */
+ * accepted [b] int32.  ws: sas_workspace_size(NULL, SAS_OP_VERIFY_DRAFTS, batch,
+ * vocab), 0 for vocabularies up to 32768. */
 sas_status sas_verify_drafts(int32_t batch, int32_t rows, int32_t vocab, int32_t max_draft, const sas_verify_in* in,
                              int32_t* out_tokens, int32_t* accepted, void* ws, size_t ws_bytes, void* stream);
 

@@ -728,8 +728,6 @@ float* carve_qk_backward(Carve& cv, const sas_config* c) {
   return (float*)cv.take((size_t)QK_BWD_GROUPS * 2 * c->head_dim * 4);
 }
 
-size_t verify_part_bytes(int b) { return (size_t)b * VERIFY_PIECES * 2 * sizeof(double); }
-
 struct ChunkWs {
   int32_t* head;
   int32_t* job_base;
@@ -1024,7 +1022,7 @@ size_t sas_workspace_size(const sas_config* c, int32_t op, int32_t batch, int32_
       carve_chunk(cv, SIZE_MAX, c, batch);
       break;
     case SAS_OP_VERIFY_DRAFTS:
-      cv.take(verify_part_bytes(batch));
+      cv.take(verify_scratch_bytes(batch, seq_len));
       break;
     case SAS_OP_LAYER_CHUNK:
       if (seq_len <= 0 || batch > CHUNK_MAX_SEQS || check_config(c, true) != SAS_OK) return 0;
@@ -1976,7 +1974,7 @@ sas_status sas_verify_drafts(int32_t batch, int32_t rows, int32_t vocab, int32_t
   SAS_TRY(check_ptr(in->u_sample, "in.u_sample", true));
   SAS_TRY(check_ptr(out_tokens, "out_tokens", true));
   SAS_TRY(check_ptr(accepted, "accepted", true));
-  SAS_TRY(check_ws(ws, ws_bytes, verify_part_bytes(batch)));
+  SAS_TRY(check_ws(ws, ws_bytes, verify_scratch_bytes(batch, vocab)));
   VerifyArgs a = {};
   a.b = batch;
   a.vocab = vocab;

@@ -458,9 +458,10 @@ struct VerifyArgs {
   const int32_t *tokens, *start;   // [rows], [b + 1]
   const float *u_accept, *u_sample;
   int32_t *out, *accepted;         // [b, max_draft + 1], [b]
-  double* part;                    // [b, VERIFY_PIECES, 2] sums of the pieces of the weights
+  double* part;                    // [b, 16, 16] sums of pieces (vocab > VERIFY_ONE)
 };
-constexpr int VERIFY_PIECES = 256, VERIFY_MIN_PIECES = 32;
+constexpr int VERIFY_ONE = 32768;  // the largest vocabulary of a single workgroup
+inline size_t verify_scratch_bytes(int b, int vocab) { return vocab > VERIFY_ONE ? (size_t)b * 256 * sizeof(double) : 0; }
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s);
 
 // ---- model_ends.hip --------------------------------------------------------

@@ -6,34 +6,40 @@
 // accepted (from p without x_j when the draft has no probabilities; from p
 // itself when nothing is left), from p after the last when all were.
 //
-// Only one row of p and one of q are read in full, b vocab (4 or 8) bytes:
-// verify_sum_kernel cuts them into pieces, a workgroup each, and leaves the pieces'
-// sums; verify_pick_kernel, a thread a piece, finds the one that the uniform falls
-// into by a prefix sum and rescans that piece alone, each thread a run of it.  Differences and sums are fp64: the
-// fp32 inputs' products and differences are exact there, and a token's border
-// in the CDF is some 1e-16 wide rather than the 1e-7 of an fp32 sum.
+// Only one row of p and one of q are read in full, b vocab (4 or 8) bytes.  The
+// vocabulary is cut in sixteen, the sixteenth that the uniform falls into in sixteen
+// again, until a wave can scan it token by token.  A workgroup a sequence does it all
+// up to VERIFY_ONE tokens; one compute unit reads some 21 GB/s, so that the sums of
+// larger vocabularies are taken by sixteen workgroups a sequence first:
+//   8 x  32000: one workgroup 12 us, two kernels 4 + 11;
+//   128 x 100003 (102 MB): one workgroup 46 us, two kernels 18 + 11.
+// Differences and sums are fp64: the fp32 inputs' products and differences are exact
+// there, and a token's border in the CDF is some 1e-16 wide rather than the 1e-7 of an
+// fp32 sum.
 #include "common.h"
 #include "kernels.h"
 
 namespace sas {
 
-constexpr int VERIFY_NT = 256;
+constexpr int VERIFY_WAVES = 16;  // and pieces of a cut
 
-// The rows that sequence i's last token is drawn from, found by the first wave.
+// tokens of a piece of n, whole steps of a wave
+__host__ __device__ __forceinline__ int verify_piece(int n) { return ((n + VERIFY_WAVES - 1) / VERIFY_WAVES + 63) / 64 * 64; }
+
+// The rows that sequence i's last token is drawn from, found by every wave.
 struct VerifyRow {
   int r0, acc;      // first drafted token, accepted ones
   const float* p;   // target row
   const float* q;   // draft row, or null
   int skip;         // token that is left out (a draft without probabilities), or -1
 };
-// `known`: the accepted tokens, or -1 to find them
-__device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i, int known) {
+__device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i) {
   const int lane = threadIdx.x & 63;
   const int r0 = min(max(P.start[i], 0), P.rows);
   const int m = min(min(max(P.start[i + 1], r0), P.rows) - r0, P.max_draft);
   // 64 drafted tokens at a time; the first that is not accepted ends the search
-  int acc = known >= 0 ? known : m;
-  for (int j0 = 0; known < 0 && j0 < m; j0 += 64) {
+  int acc = m;
+  for (int j0 = 0; j0 < m; j0 += 64) {
     const int j = j0 + lane;
     bool ok = true;
     if (j < m) {
@@ -61,10 +67,10 @@ __device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i, int 
   return v;
 }
 
-// weights of token e: (left over, target); negative and NaN values count as zero
-__device__ __forceinline__ double verify_pos(double x) { return x > 0.0 ? x : 0.0; }
-__device__ __forceinline__ double verify_left(const VerifyRow& v, int e, float p, float q) {
-  return e == v.skip ? 0.0 : verify_pos((double)p - (double)q);
+// weight of token e (negative and NaN ones count as zero)
+__device__ __forceinline__ double verify_weight(const VerifyRow& v, int e) {
+  const double w = (double)v.p[e] - (v.q ? (double)v.q[e] : 0.0);
+  return e != v.skip && w > 0.0 ? w : 0.0;
 }
 
 __device__ __forceinline__ double wave_sum_f64(double x) {
@@ -73,124 +79,142 @@ __device__ __forceinline__ double wave_sum_f64(double x) {
   return x;
 }
 
-__global__ void __launch_bounds__(VERIFY_NT) verify_sum_kernel(VerifyArgs P, int len) {
-  __shared__ double red[2][VERIFY_NT / 64];
-  const int i = blockIdx.y, piece = blockIdx.x;
-  const VerifyRow v = verify_row(P, i, -1);
-  if (piece == 0 && threadIdx.x == 0) P.accepted[i] = v.acc;
-  const int e0 = piece * len, e1 = min(e0 + len, P.vocab);
-  double left = 0.0, all = 0.0;
-  for (int e = e0 + threadIdx.x; e < e1; e += VERIFY_NT) {
-    const float p = v.p[e], q = v.q ? v.q[e] : 0.f;
-    left += verify_left(v, e, p, q);
-    all += verify_pos((double)p);
+// sum of the weights of tokens [a, b), a lane every 64th
+__device__ __forceinline__ double verify_sum(const VerifyRow& v, int a, int b) {
+  double w[4] = {0.0, 0.0, 0.0, 0.0};
+  int e = a + (threadIdx.x & 63);
+  // eight tokens' loads together
+  for (; e + 7 * 64 < b; e += 8 * 64) {
+    double x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = verify_weight(v, e + u * 64);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) w[u & 3] += x[u];
   }
-  left = wave_sum_f64(left);
-  all = wave_sum_f64(all);
-  if ((threadIdx.x & 63) == 0) {
-    red[0][threadIdx.x >> 6] = left;
-    red[1][threadIdx.x >> 6] = all;
-  }
+  for (; e < b; e += 64) w[0] += verify_weight(v, e);
+  return wave_sum_f64((w[0] + w[1]) + (w[2] + w[3]));
+}
+
+// Sums of the sixteen pieces of [e0, e1), `len` tokens each, into s.
+__device__ __forceinline__ void verify_sums(const VerifyRow& v, int e0, int e1, int len, double* s) {
+  const int wave = threadIdx.x >> 6;
+  const int a = (int)min((long long)e0 + (long long)wave * len, (long long)e1);
+  const double sum = verify_sum(v, a, (int)min((long long)a + len, (long long)e1));
   __syncthreads();
-  if (threadIdx.x < 2) {
-    double t = 0.0;
-    for (int w = 0; w < VERIFY_NT / 64; ++w) t += red[threadIdx.x][w];
-    P.part[((size_t)i * gridDim.x + piece) * 2 + threadIdx.x] = t;
+  if ((threadIdx.x & 63) == 0) s[wave] = sum;
+  __syncthreads();
+}
+
+// part[i][k][j]: the sum of piece j of piece k; workgroup (k, i), a wave four of them
+__global__ void __launch_bounds__(256) verify_sum_kernel(VerifyArgs P) {
+  const int k = blockIdx.x, i = blockIdx.y, wave = threadIdx.x >> 6;
+  const VerifyRow v = verify_row(P, i);
+  const int len = verify_piece(P.vocab), sub = verify_piece(len);
+  const int e0 = (int)min((long long)k * len, (long long)P.vocab), e1 = (int)min((long long)e0 + len, (long long)P.vocab);
+  for (int j = wave * 4; j < wave * 4 + 4; ++j) {
+    const int a = (int)min((long long)e0 + (long long)j * sub, (long long)e1);
+    const double sum = verify_sum(v, a, (int)min((long long)a + sub, (long long)e1));
+    if ((threadIdx.x & 63) == 0) P.part[((size_t)i * VERIFY_WAVES + k) * VERIFY_WAVES + j] = sum;
   }
 }
 
-// sum before this thread of v over the workgroup, and the whole (s: 4 values of LDS)
-__device__ __forceinline__ double scan_f64(double v, double* s, double& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
+// SUMS: verify_sum_kernel has taken the sums of the first two cuts
+template <bool SUMS>
+__global__ void __launch_bounds__(VERIFY_WAVES * 64) verify_kernel(VerifyArgs P) {
+  __shared__ double s[VERIFY_WAVES], part[SUMS ? VERIFY_WAVES : 1][VERIFY_WAVES];
+  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  if constexpr (SUMS) {
+    if (tid < VERIFY_WAVES * VERIFY_WAVES)
+      part[tid / VERIFY_WAVES][tid % VERIFY_WAVES] = P.part[(size_t)i * VERIFY_WAVES * VERIFY_WAVES + tid];
   }
-  __syncthreads();
-  if (lane == 63) s[wave] = x;
-  __syncthreads();
-  double at = 0.0, sum = 0.0;
-#pragma unroll
-  for (int w = 0; w < VERIFY_NT / 64; ++w) {
-    if (w < wave) at += s[w];
-    sum += s[w];
+  VerifyRow v = verify_row(P, i);
+  int e0 = 0, e1 = P.vocab, len = verify_piece(P.vocab);
+  if constexpr (SUMS) {
+    __syncthreads();
+    if (tid < VERIFY_WAVES) {
+      double x = 0.0;
+      for (int j = 0; j < VERIFY_WAVES; ++j) x += part[tid][j];
+      s[tid] = x;
+    }
+    __syncthreads();
+  } else {
+    verify_sums(v, e0, e1, len, s);
   }
-  total = sum;
-  x = __shfl_up(x, 1, 64);
-  return at + (lane ? x : 0.0);
-}
-
-__global__ void __launch_bounds__(VERIFY_NT) verify_pick_kernel(VerifyArgs P, int len, int pieces) {
-  __shared__ double s[VERIFY_NT / 64];
-  __shared__ int hit, some;  // the first piece or token past the uniform, the last of any weight
-  __shared__ double base_s[VERIFY_NT];
-  const int i = blockIdx.x, tid = threadIdx.x;
-  const double* part = P.part + (size_t)i * pieces * 2;
-  const double w0 = tid < pieces ? part[2 * tid] : 0.0, w1 = tid < pieces ? part[2 * tid + 1] : 0.0;
-  VerifyRow v = verify_row(P, i, P.accepted[i]);
-  if (tid == 0) {
-    hit = 0x7fffffff;
-    some = -1;
-  }
-  double left, all;
-  const double b0 = scan_f64(w0, s, left), b1 = scan_f64(w1, s, all);
-  if (!(left > 0.0)) {  // nothing left over: the target itself
+  double total = 0.0;
+  for (int k = 0; k < VERIFY_WAVES; ++k) total += s[k];
+  bool known = SUMS;  // part holds the sums of the next cut
+  if (!(total > 0.0) && (v.q || v.skip >= 0)) {  // nothing left over: the target itself
     v.q = nullptr;
     v.skip = -1;
+    known = false;
+    verify_sums(v, e0, e1, len, s);
+    for (int k = 0; k < VERIFY_WAVES; ++k) total += s[k];
   }
-  const double w = left > 0.0 ? w0 : w1, before = left > 0.0 ? b0 : b1;
-  const double aim = (double)P.u_sample[i] * (left > 0.0 ? left : all);
-  base_s[tid] = before;
-  if (w > 0.0) {
-    if (before + w > aim) atomicMin(&hit, tid);
-    atomicMax(&some, tid);
-  }
-  __syncthreads();
-  const int piece = hit != 0x7fffffff ? hit : some;
-  __syncthreads();
-  if (tid == 0) {
-    hit = 0x7fffffff;
-    some = -1;
-  }
-  if (piece >= 0) {
-    // thread t's run of the piece: len / 256 tokens
-    const int run = len / VERIFY_NT, e0 = piece * len + tid * run, e1 = min(e0 + run, P.vocab);
-    double sum = 0.0, total;
-    for (int e = e0; e < e1; ++e) sum += verify_left(v, e, v.p[e], v.q ? v.q[e] : 0.f);
-    double at = base_s[piece] + scan_f64(sum, s, total);
-    if (sum > 0.0) {
-      int first = 0x7fffffff, last = -1;
-      for (int e = e0; e < e1; ++e) {
-        const double x = verify_left(v, e, v.p[e], v.q ? v.q[e] : 0.f);
-        if (!(x > 0.0)) continue;
-        at += x;
-        if (first == 0x7fffffff && at > aim) first = e;
-        last = e;
+  const double aim = (double)P.u_sample[i] * total;
+  // the piece that the aim falls into: the first whose end lies past it, or the last of
+  // any weight (sums of other pieces may differ in their last bits)
+  double before = 0.0;
+  int token = -1;
+  if (total > 0.0) {
+    for (;;) {
+      int pick = -1;
+      double at = before, to = before;
+      for (int k = 0; k < VERIFY_WAVES; ++k) {
+        if (!(s[k] > 0.0)) continue;
+        pick = k;
+        at = to;
+        to += s[k];
+        if (to > aim) break;
       }
-      if (first != 0x7fffffff) atomicMin(&hit, first);
-      atomicMax(&some, last);
+      if (pick < 0) break;  // (not reached: some piece has weight)
+      before = at;
+      e0 += pick * len;
+      e1 = min(e0 + len, e1);
+      if (e1 - e0 <= 512) break;
+      const int whole = len;
+      len = verify_piece(known ? whole : e1 - e0);
+      if (known) {
+        __syncthreads();  // (every thread has read s)
+        if (tid < VERIFY_WAVES) s[tid] = part[SUMS ? pick : 0][tid];
+        __syncthreads();
+        known = false;
+      } else {
+        verify_sums(v, e0, e1, len, s);
+      }
+    }
+    // token by token, 64 at a time
+    for (int b0 = e0; b0 < e1; b0 += 64) {
+      const int e = b0 + lane;
+      const double w = e < e1 ? verify_weight(v, e) : 0.0;
+      double x = w;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+      }
+      const unsigned long long any = __builtin_amdgcn_ballot_w64(w > 0.0);
+      const unsigned long long hit = __builtin_amdgcn_ballot_w64(w > 0.0 && before + x > aim);
+      if (any) token = b0 + 63 - __builtin_clzll(any);
+      if (hit) {
+        token = b0 + __builtin_ctzll(hit);
+        break;
+      }
+      before += __shfl(x, 63, 64);
     }
   }
-  __syncthreads();
   const int W = P.max_draft + 1;
-  for (int j = tid; j < W; j += VERIFY_NT) {
-    int t = -1;
-    if (j < v.acc) t = P.tokens[v.r0 + j];
-    else if (j == v.acc) t = hit != 0x7fffffff ? hit : some;
-    P.out[(size_t)i * W + j] = t;
-  }
+  for (int j = tid; j < W; j += VERIFY_WAVES * 64)
+    P.out[(size_t)i * W + j] = j < v.acc ? P.tokens[v.r0 + j] : j == v.acc ? token : -1;
+  if (tid == 0) P.accepted[i] = v.acc;
 }
 
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s) {
-  // pieces of whole 256-token steps, at most a thread of the second kernel each: enough
-  // workgroups to read the rows from the whole chip, and no more, since each looks the
-  // accepted tokens up first
-  const int steps = cdiv(a.vocab, VERIFY_NT), want = std::max(VERIFY_MIN_PIECES, std::min(VERIFY_PIECES, 2048 / a.b));
-  const int len = cdiv(steps, std::min(steps, want)) * VERIFY_NT, pieces = cdiv(a.vocab, len);
-  verify_sum_kernel<<<dim3(pieces, a.b), VERIFY_NT, 0, s>>>(a, len);
-  verify_pick_kernel<<<a.b, VERIFY_NT, 0, s>>>(a, len, pieces);
+  if (a.vocab <= VERIFY_ONE) {
+    verify_kernel<false><<<a.b, VERIFY_WAVES * 64, 0, s>>>(a);
+  } else {
+    verify_sum_kernel<<<dim3(VERIFY_WAVES, a.b), 256, 0, s>>>(a);
+    verify_kernel<true><<<a.b, VERIFY_WAVES * 64, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 

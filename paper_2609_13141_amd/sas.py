@@ -24,8 +24,8 @@ GATE_POS = {"inner": 0, "outer": 1}
 GATE_ACT = {"softmax": 0, "sigmoid": 1, "raw": 2}
 SCOPES = {"sparse": 0, "full": 1}
 (OP_ATTENTION, OP_MLP, OP_LAYER, OP_DECODE, OP_LM_HEAD, OP_DECODE_SELECT, OP_ATTENTION_BACKWARD,
- OP_SELECTOR_BACKWARD, OP_SELECTION_STATS, OP_QK_BACKWARD, OP_ATTENTION_CHUNK, OP_VERIFY_DRAFTS,
- OP_LAYER_CHUNK) = range(13)
+ OP_SELECTOR_BACKWARD, OP_SELECTION_STATS, OP_QK_BACKWARD, OP_ATTENTION_CHUNK, OP_LAYER_CHUNK,
+ OP_VERIFY_DRAFTS) = range(13)
 TORCH_DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 EXPORTS = ("sas_workspace_size", "sas_attention_prefill", "sas_mlp_forward", "sas_layer_forward",
@@ -818,9 +818,10 @@ def verify_drafts(target, draft, tokens, draft_start, u_accept, u_sample, max_dr
                   _need("u_sample", u_sample, f32, (b,), dev))
     out = {"tokens": torch.empty(b, max_draft + 1, dtype=i32, device=dev),
            "accepted": torch.empty(b, dtype=i32, device=dev)}
-    buf = _scratch(ws, lib().sas_workspace_size(None, OP_VERIFY_DRAFTS, b, 0), dev)
+    nbytes = lib().sas_workspace_size(None, OP_VERIFY_DRAFTS, b, V)
+    buf = _scratch(ws, nbytes, dev) if nbytes else None
     _call(dev, lib().sas_verify_drafts, b, rows, V, max_draft, C.byref(vi), out["tokens"].data_ptr(),
-          out["accepted"].data_ptr(), buf.data_ptr(), buf.numel())
+          out["accepted"].data_ptr(), _ptr(buf), nbytes)
     return out
 
 

@@ -38,7 +38,7 @@ def check(args, D):
     return want, acc
 
 
-@pytest.mark.parametrize("V", [1, 2, 255, 256, 257, 1000, 32000, 100003])
+@pytest.mark.parametrize("V", [1, 2, 255, 256, 257, 1000, 8193, 32768, 32769, 100003])
 @pytest.mark.parametrize("drafts", [[3], [0], [0, 1, 5, 2, 7], [4] * 40], ids=str)
 @pytest.mark.parametrize("with_q", [True, False])
 def test_against_the_oracle(V, drafts, with_q):
