@@ -92,39 +92,55 @@ __device__ __forceinline__ ChunkWork chunk_work(const ChunkArgs& P, const ChunkS
   w.prow = min(q.m, qpt) * G;
   return w;
 }
-__device__ __forceinline__ int chunk_parts(int nk, int C) { return max(1, (int)(((long long)nk + C - 1) / C)); }
+__device__ __forceinline__ int chunk_parts(int nk, int C) { return max(1, (int)(((uint32_t)nk + (uint32_t)C - 1) / (uint32_t)C)); }
 
 // The length C of a part, in key tiles.  With fewer (tile, head) pairs than resident
 // workgroups, the least C whose parts still fit them: one round of jobs, none longer
 // than it has to be.  With more, a part is the average work of a workgroup, which
 // only cuts tiles far longer than the others.  A divided tile has at most 2 nk / C
 // parts, so that C >= 2 sum(units nk prow) / part_rows keeps them inside the scratch.
-// sum(f): the sum over all sequences of f of their work, the same in every thread.
+// sum(f): the sum over all sequences of f of their work, the same in every thread (in
+// fp64, exact up to 2^53; a sequence counts for at most 2^20 parts).
 template <typename Sum>
 __device__ __forceinline__ int chunk_part_length(const ChunkArgs& P, int res, Sum sum) {
   if (P.part_rows <= 0) return 0x7fffffff;
-  const long long U = sum([](const ChunkWork& w) { return (long long)w.units; });
-  const long long W = sum([](const ChunkWork& w) { return (long long)w.units * w.nk; });
-  const long long R = sum([](const ChunkWork& w) { return (long long)w.units * w.nk * w.prow; });
-  const long long least = max((long long)CHUNK_MIN_TILES, (2 * R + P.part_rows - 1) / P.part_rows);
-  long long lo = max(least, (W + res - 1) / res);
+  const double U = sum([](const ChunkWork& w) { return (double)w.units; });
+  const double W = sum([](const ChunkWork& w) { return (double)w.units * w.nk; });
+  const double R = sum([](const ChunkWork& w) { return (double)w.units * w.nk * w.prow; });
+  const double least = fmax((double)CHUNK_MIN_TILES, ceil(2.0 * R / (double)P.part_rows));
+  int lo = (int)fmin(fmax(least, ceil(W / res)), 0x3fffffff);
   if (U < res) {
     // W / C + U parts at most: some C up to W / (res - U) fits
-    long long hi = max(lo, (W + res - U - 1) / (res - U));
+    int hi = max(lo, (int)fmin(ceil(W / (res - U)), 0x3fffffff));
     while (lo < hi) {
-      const long long mid = (lo + hi) / 2;
-      const int C = (int)min(mid, 0x7fffffffll);
-      if (sum([C](const ChunkWork& w) { return (long long)w.units * chunk_parts(w.nk, C); }) <= res) hi = mid;
-      else lo = mid + 1;
+      const int C = (lo + hi) / 2;
+      if (sum([C](const ChunkWork& w) { return (double)min((long long)w.units * chunk_parts(w.nk, C), 1ll << 20); }) <= res) hi = C;
+      else lo = C + 1;
     }
   }
-  return (int)min(lo, 0x7fffffffll);
+  return lo;
 }
 
-__device__ __forceinline__ long long wave_sum_i64(long long v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+// sum over the wave by data-parallel moves: an inclusive sum within rows of 16, then
+// the rows' last lanes
+__device__ __forceinline__ double wave_total(double v) {
+#define CHUNK_DPP_ADD(ctrl, rows)                                                                     \
+  {                                                                                                   \
+    const long long b = __double_as_longlong(v);                                                      \
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, ctrl, rows, 0xf, false);          \
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), ctrl, rows, 0xf, false);  \
+    v += __longlong_as_double((long long)((uint64_t)(uint32_t)lo | (uint64_t)(uint32_t)hi << 32));    \
+  }
+  CHUNK_DPP_ADD(0x111, 0xf)
+  CHUNK_DPP_ADD(0x112, 0xf)
+  CHUNK_DPP_ADD(0x114, 0xf)
+  CHUNK_DPP_ADD(0x118, 0xf)
+  CHUNK_DPP_ADD(0x142, 0xa)
+  CHUNK_DPP_ADD(0x143, 0xc)
+#undef CHUNK_DPP_ADD
+  const long long b = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, 63), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+  return __longlong_as_double((long long)((uint64_t)lo | (uint64_t)hi << 32));
 }
 
 // sum over the workgroup's 1024 threads of v, and the sum before this thread (s: 16 values of LDS)
@@ -163,11 +179,12 @@ __global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_
     w[u] = u < per && i < P.b ? chunk_work(P, chunk_seq(P, i), keys_per_tile) : ChunkWork{0, 0, 0};
   }
   const int C = chunk_part_length(P, res, [&](auto f) {
-    long long v = 0, total;
+    double v = 0.0;
 #pragma unroll
     for (int u = 0; u < MAX_PER; ++u) v += f(w[u]);
-    (void)scan1024(v, s, total);
-    return total;
+    long long total;
+    (void)scan1024((long long)v, s, total);  // (whole numbers)
+    return (double)total;
   });
   long long jobs = 0, prows = 0;
 #pragma unroll
@@ -204,7 +221,7 @@ struct ChunkJob {
 __device__ __forceinline__ ChunkJob chunk_wave_plan(const ChunkArgs& P, int keys_per_tile, int res, int block) {
   const int lane = threadIdx.x & 63;
   const ChunkWork w = lane < P.b ? chunk_work(P, chunk_seq(P, lane), keys_per_tile) : ChunkWork{0, 0, 0};
-  const int C = chunk_part_length(P, res, [&](auto f) { return wave_sum_i64(f(w)); });
+  const int C = chunk_part_length(P, res, [&](auto f) { return wave_total(f(w)); });
   const int parts = chunk_parts(w.nk, C);
   const int jobs = w.units * parts, prows = parts > 1 ? jobs * w.prow : 0;
   int j = jobs, r = prows;
