@@ -612,7 +612,7 @@ sas_status sas_cache_append(const sas_config* cfg, int32_t batch, int32_t rows, 
  * q, o [rows, H, dh]; lse [rows, H] fp32 or NULL.  A row that attends nothing
  * gives o = 0, lse = -inf.  H / Hkv <= 128; the block table covers at most 2^30
  * positions.  ws: sas_workspace_size(cfg, SAS_OP_ATTENTION_CHUNK, batch, rows),
- * of which all but the last 69 MiB (fewer for dh = 64), where parts of divided
+ * of which all but the last 65 MiB (fewer for dh = 64), where parts of divided
  * work are joined, is needed. */
 sas_status sas_attention_chunk(const sas_config* cfg, int32_t batch, int32_t rows, const void* q,
                                const int32_t* row_start, const int32_t* kv_len, const sas_paged_kv* cache, void* o,

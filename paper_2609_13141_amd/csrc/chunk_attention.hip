@@ -35,10 +35,13 @@ constexpr float LN2 = 0.6931471805599453f;
 
 typedef __attribute__((address_space(3))) void chunk_lds_t;
 
-// Keys of a tile: 64 in bf16, 32 in fp32 (the same bytes).
+// Keys of a tile: 64 in bf16, 32 in fp32 (the same bytes).  LEAST: tiles of the shortest
+// part.  An fp32 tile takes 2.9 us, more than another part's merge: 4 sequences of up to 60
+// new tokens over up to 200 keys take 14.8 us with parts of one tile and 16.3 with two.  A
+// bf16 tile takes less, and parts of one tile gained nothing.
 template <typename T> struct ChunkTile;
-template <> struct ChunkTile<bf16_t> { static constexpr int KEYS = 64; };
-template <> struct ChunkTile<float> { static constexpr int KEYS = 32; };
+template <> struct ChunkTile<bf16_t> { static constexpr int KEYS = 64, LEAST = 2; };
+template <> struct ChunkTile<float> { static constexpr int KEYS = 32, LEAST = 1; };
 
 // position of 16-byte chunk c of tile row r (bank-conflict-free for the reads below)
 template <typename T, int DH>
@@ -102,12 +105,12 @@ __device__ __forceinline__ int chunk_parts(int nk, int C) { return max(1, (int)(
 // sum(f): the sum over all sequences of f of their work, the same in every thread (in
 // fp64, exact up to 2^53; a sequence counts for at most 2^20 parts).
 template <typename Sum>
-__device__ __forceinline__ int chunk_part_length(const ChunkArgs& P, int res, Sum sum) {
+__device__ __forceinline__ int chunk_part_length(const ChunkArgs& P, int least_tiles, int res, Sum sum) {
   if (P.part_rows <= 0) return 0x7fffffff;
   const double U = sum([](const ChunkWork& w) { return (double)w.units; });
   const double W = sum([](const ChunkWork& w) { return (double)w.units * w.nk; });
   const double R = sum([](const ChunkWork& w) { return (double)w.units * w.nk * w.prow; });
-  const double least = fmax((double)CHUNK_MIN_TILES, ceil(2.0 * R / (double)P.part_rows));
+  const double least = fmax((double)least_tiles, ceil(2.0 * R / (double)P.part_rows));
   int lo = (int)fmin(fmax(least, ceil(W / res)), 0x3fffffff);
   if (U < res) {
     // W / C + U parts at most: some C up to W / (res - U) fits
@@ -168,7 +171,7 @@ __device__ __forceinline__ long long scan1024(long long v, long long* s, long lo
 // One workgroup: divides the work of any number of sequences and clears the job queues.
 // head[0] = jobs, head[1] = whether a tile is divided, head[8 + x] = the next job of
 // XCD x's share.
-__global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_per_tile, int res) {
+__global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_per_tile, int least_tiles, int res) {
   __shared__ long long s[16];
   constexpr int MAX_PER = CHUNK_MAX_SEQS / 1024;
   const int tid = threadIdx.x, per = (P.b + 1023) / 1024;
@@ -178,7 +181,7 @@ __global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_
     const int i = tid * per + u;
     w[u] = u < per && i < P.b ? chunk_work(P, chunk_seq(P, i), keys_per_tile) : ChunkWork{0, 0, 0};
   }
-  const int C = chunk_part_length(P, res, [&](auto f) {
+  const int C = chunk_part_length(P, least_tiles, res, [&](auto f) {
     double v = 0.0;
 #pragma unroll
     for (int u = 0; u < MAX_PER; ++u) v += f(w[u]);
@@ -218,10 +221,10 @@ struct ChunkJob {
   int seq, rel;
   int2 sp;
 };
-__device__ __forceinline__ ChunkJob chunk_wave_plan(const ChunkArgs& P, int keys_per_tile, int res, int block) {
+__device__ __forceinline__ ChunkJob chunk_wave_plan(const ChunkArgs& P, int keys_per_tile, int least_tiles, int res, int block) {
   const int lane = threadIdx.x & 63;
   const ChunkWork w = lane < P.b ? chunk_work(P, chunk_seq(P, lane), keys_per_tile) : ChunkWork{0, 0, 0};
-  const int C = chunk_part_length(P, res, [&](auto f) { return wave_total(f(w)); });
+  const int C = chunk_part_length(P, least_tiles, res, [&](auto f) { return wave_total(f(w)); });
   const int parts = chunk_parts(w.nk, C);
   const int jobs = w.units * parts, prows = parts > 1 ? jobs * w.prow : 0;
   int j = jobs, r = prows;
@@ -899,7 +902,7 @@ __global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P, int res
   const int lane = threadIdx.x & 63;
   if constexpr (INLINE) {
     if (threadIdx.x < 64) {
-      const ChunkJob j = chunk_wave_plan(P, ChunkTile<T>::KEYS, res, blockIdx.x);
+      const ChunkJob j = chunk_wave_plan(P, ChunkTile<T>::KEYS, ChunkTile<T>::LEAST, res, blockIdx.x);
       if (lane == 0) job_s = j;
     }
   }
@@ -1046,7 +1049,8 @@ static ChunkKernels chunk_kernels() {
 
 hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) {
   const int G = a.H / a.Hkv;
-  const int keys = dtype == SAS_BF16 ? 64 : 32;
+  const int keys = dtype == SAS_BF16 ? ChunkTile<bf16_t>::KEYS : ChunkTile<float>::KEYS;
+  const int least = dtype == SAS_BF16 ? ChunkTile<bf16_t>::LEAST : ChunkTile<float>::LEAST;
   // the pipelined kernel where the average sequence fills a tile: with fewer rows the
   // keys' bytes bound the call
   const bool piped = dtype == SAS_BF16 && (long long)a.rows * G > (long long)CHUNK_ROWS * std::min(a.b, a.rows);
@@ -1060,11 +1064,11 @@ hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) 
   if (res <= 0) return hipErrorInvalidValue;
   // the most jobs that there can be: tiles in parts of the least length
   const long long max_keys = (long long)a.max_pages << a.ps_shift;
-  const long long part_keys = (long long)keys * CHUNK_MIN_TILES;
+  const long long part_keys = (long long)keys * least;
   const long long parts = a.part_rows > 0 ? (max_keys + part_keys - 1) / part_keys : 1;
   const long long most = (std::min<long long>(res, tiles * std::min<long long>(parts, res)) + ATTN_XCDS - 1) / ATTN_XCDS * ATTN_XCDS;
   const bool inl = a.b <= 64 && tiles < res;
-  if (!inl) chunk_plan_kernel<<<1, 1024, 0, s>>>(a, keys, res);
+  if (!inl) chunk_plan_kernel<<<1, 1024, 0, s>>>(a, keys, least, res);
   (inl ? k.inl : k.queued)<<<(unsigned)most, 256, 512 * a.dh, s>>>(a, res);
   if (parts > 1) {
     const long long waves = (long long)a.rows * a.H;

@@ -447,7 +447,6 @@ constexpr int CHUNK_ROWS = 128;  // rows of a tile
 // which is the most that parts of the average work of a workgroup can come to, of 128
 // rows.
 constexpr long long CHUNK_PART_ROWS = 1024 * CHUNK_ROWS;
-constexpr int CHUNK_MIN_TILES = 2;  // key tiles of the least part
 constexpr long long CHUNK_MAX_KEYS = 1ll << 30;  // positions that a block table may cover
 hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s);
 
