@@ -569,7 +569,8 @@ typedef struct {
 
 /* Rows of query, key and value heads: q [rows, H, dh], k, v [rows, Hkv, dh] with
  * q_stride .. elements from row to row (0 = contiguous; otherwise a multiple of 16
- * bytes), such as the columns of one packed projection. */
+ * bytes, and rows do not overlap), such as the columns of one packed projection.
+ * Fewer than 2^25 rows and 2^30 heads in all. */
 typedef struct {
   const void* q;
   const void* k;
@@ -596,8 +597,8 @@ sas_status sas_qk_norm_rope_backward(const sas_config* cfg, int32_t rows, const 
 
 /* A chunk's heads into the cache: q_out as sas_qk_norm_rope; the normed and
  * rotated k and v as it is go to the pages at slot [rows] (int64 DEVICE; a slot
- * outside the pool drops the row's key and value; of two rows with one slot
- * either may stay); then the summaries of the blocks that positions
+ * outside the pool drops the row's key and value; of two rows with one slot any
+ * head's key and value may be either's); then the summaries of the blocks that positions
  * ctx_len[i] .. kv_len[i] - 1 complete are written to cache->k_summary (mean of
  * the block's keys in the pages, projected by w_gk [Hkv, dh, dh] when given).
  * q_out may be in->q itself when that is contiguous. */
@@ -609,7 +610,7 @@ sas_status sas_cache_append(const sas_config* cfg, int32_t batch, int32_t rows, 
  * (appended before) among them: row j of sequence i's m rows is at position
  * t = kv_len[i] - m + j and attends every mapped position up to t (the dense
  * prefill of Sec. 5.1 over a cache; cfg->mode is not read).
- * q, o [rows, H, dh]; lse [rows, H] fp32 or NULL.  A row that attends nothing
+ * q, o [rows, H, dh], apart; lse [rows, H] fp32 or NULL.  A row that attends nothing
  * gives o = 0, lse = -inf.  H / Hkv <= 128; the block table covers at most 2^30
  * positions.  ws: sas_workspace_size(cfg, SAS_OP_ATTENTION_CHUNK, batch, rows),
  * of which all but the last 65 MiB (fewer for dh = 64), where parts of divided

@@ -790,9 +790,10 @@ sas_status qk_args(const sas_config* c, int32_t rows, const sas_rotary* rot, con
   if (!(c->rms_eps >= 0.f)) return fail(SAS_ERR_INVALID_ARGUMENT, "rms_eps must be >= 0");
   if (!(c->rope_base > 0.f)) return fail(SAS_ERR_INVALID_ARGUMENT, "rope_base must be > 0");
   if (rows <= 0) return fail(SAS_ERR_INVALID_ARGUMENT, "rows %d must be positive", rows);
-  if ((long long)rows * (c->n_heads + 2ll * c->n_kv_heads) > INT32_MAX)
-    return fail(SAS_ERR_UNSUPPORTED, "%d rows of %d/%d heads (supported: fewer than 2^31 heads)", rows, c->n_heads,
-                c->n_kv_heads);
+  // (fewer than 2^32 threads in a launch: 64 for each row and for each further 32 heads of one)
+  if (rows >= 1 << 25 || (long long)rows * (c->n_heads + 2ll * c->n_kv_heads) >= 1 << 30)
+    return fail(SAS_ERR_UNSUPPORTED, "%d rows of %d/%d heads (supported: fewer than 2^25 rows and 2^30 heads)", rows,
+                c->n_heads, c->n_kv_heads);
   if (!rot || !in) return fail(SAS_ERR_INVALID_ARGUMENT, "rot/in is NULL");
   SAS_TRY(check_ptr(rot->gain_q, "rot.gain_q", false));
   SAS_TRY(check_ptr(rot->gain_k, "rot.gain_k", false));
@@ -1878,6 +1879,7 @@ sas_status sas_attention_chunk(const sas_config* c, int32_t batch, int32_t rows,
   Carve cv(ws);
   const ChunkWs w = carve_chunk(cv, ws_bytes, c, batch);
   SAS_TRY(check_ws(ws, ws_bytes, w.need));
+  if (o == q) return fail(SAS_ERR_INVALID_ARGUMENT, "o is q");
   return run_chunk_attention(c, batch, rows, q, row_start, kv_len, cache, o, lse, w, (hipStream_t)stream);
 }
 

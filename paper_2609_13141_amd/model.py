@@ -91,9 +91,9 @@ class Stack:
         x = sas.embed(self.cfg_prefill, ids.view(1, -1), self.ends["embed"])[0]
         none = torch.zeros(1, dtype=torch.int32, device=ids.device)
         plan = None
+        # (every position's page is there already, in another order in each layer)
+        held = torch.full_like(ctx_len, self.caches[0].block_table.shape[1])
         for W, cache in zip(self.layers, self.caches):
-            # (every position's page is there already, in another order in each layer)
-            held = torch.full_like(ctx_len, cache.block_table.shape[1])
             plan = sas.plan_chunk(cache, ctx_len, new_len, held, none, none, ids.numel())
             x = sas.layer_chunk(self.cfg_prefill, x, W, cache, ctx_len, plan, ws=self.ws)
         return x, plan

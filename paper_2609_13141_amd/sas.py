@@ -598,6 +598,13 @@ def _need(name: str, t, dtype, shape: tuple, dev) -> int:
     _refuse(name, f"contiguous {dtype} {list(shape)} on {dev}", t)
 
 
+def _count(name: str, n: int, least: int = 0) -> int:
+    """n, where it fits the C argument."""
+    if not least <= n < 2 ** 31:
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name} {n} (from {least} to 2^31 - 1)")
+    return n
+
+
 def _device(name: str, t):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name} is not a tensor on the GPU")
@@ -644,6 +651,8 @@ def _heads_arg(cfg: Config, name: str, t, heads: int, rows: int, dev):
     st = t.stride()
     if st[2] != 1 or (heads > 1 and st[1] != dh):
         _refuse(name, "rows of contiguous heads", t)
+    if rows > 1 and st[0] < heads * dh:  # (expanded or overlapping rows)
+        _refuse(name, "rows that do not overlap", t)
     return t.data_ptr(), st[0] if rows > 1 else heads * dh
 
 
@@ -665,6 +674,7 @@ def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free
     of cache.block_table and returns row_start [b+1], kv_len [b], seq and pos
     [rows], slot [rows] (int64), pages_held [b], free_count [1], missing [1]."""
     dev = _device("ctx_len", ctx_len)
+    _count("rows", rows, 1)
     b = ctx_len.numel()
     i32 = torch.int32
     table = cache.block_table
@@ -672,9 +682,7 @@ def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free
                  cache.page_size, table.shape[1], 0)
     pi = PlanIn(_need("ctx_len", ctx_len, i32, (b,), dev), _need("new_len", new_len, i32, (b,), dev),
                 _need("pages_held", pages_held, i32, (b,), dev), _need("free_pages", free_pages, i32, (free_pages.numel(),), dev),
-                _need("free_count", free_count, i32, (1,), dev), free_pages.numel())
-    if rows <= 0:
-        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"rows {rows} must be positive")
+                _need("free_count", free_count, i32, (1,), dev), _count("entries of free_pages", free_pages.numel()))
     # one allocation for the int32 outputs, each at a multiple of 16 bytes
     sizes, names = [], []
     for name, n in (("seq", rows), ("pos", rows), ("kv_len", b), ("pages_held", b), ("row_start", b + 1),
@@ -808,8 +816,7 @@ def verify_drafts(target, draft, tokens, draft_start, u_accept, u_sample, max_dr
     dev = _device("target", target)
     rows, b = tokens.numel(), u_sample.numel()
     f32, i32 = torch.float32, torch.int32
-    if max_draft < 0:
-        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"max_draft {max_draft} is negative")
+    _count("max_draft", max_draft), _count("rows", rows)
     V = target.shape[-1]
     tp = _need("target", target, f32, (rows + b, V), dev)
     dp = None if draft is None else _need("draft", draft, f32, (rows, V), dev)

@@ -63,7 +63,8 @@ QK = [
     (dict(rot=rotary(section=(63, 0, 0))), BAD, b"pairs"), (dict(rot=rotary(3, (65, -1, 0))), BAD, b"section"),
     (dict(rot=rotary(pos=None)), BAD, b"rot.pos"), (dict(rot=rotary(gain_k=0x1004)), BAD, b"aligned"),
     (dict(x=qkv(q=None)), BAD, b"in.q"), (dict(x=qkv(qs=8)), BAD, b"q_stride"), (dict(x=qkv(ks=261)), BAD, b"k_stride"),
-    (dict(x=qkv(qs=-512)), BAD, b"q_stride"), (dict(rows=2 ** 30), UNSUP, b"2^31"), (dict(x=qkv(qs=2 ** 61)), BAD, b"q_stride"),
+    (dict(x=qkv(qs=-512)), BAD, b"q_stride"), (dict(rows=2 ** 30), UNSUP, b"2^30"),
+    (dict(rows=2 ** 27, cfg=dict(n_heads=2)), UNSUP, b"2^25 rows"), (dict(x=qkv(qs=2 ** 61)), BAD, b"q_stride"),
     (dict(cfg=dict(rope_base=0.0)), BAD, b"rope_base"), (dict(cfg=dict(rms_eps=-1.0)), BAD, b"rms_eps"),
     (dict(cfg=dict(head_dim=96)), UNSUP, b"head_dim"), (dict(rot=None), BAD, b"NULL"),
 ]
@@ -126,6 +127,7 @@ def test_attention(L):
     assert call(cache=kv(page_size=12)) == BAD
     assert call(rows=2 ** 29) == UNSUP
     assert call(ws=None) == WS and call(n=64) == WS
+    assert call() == BAD and b"o is q" in L.sas_last_error()   # (q and o are both P)
     assert sas.workspace_size(cfg, sas.OP_ATTENTION_CHUNK, 4097, 1) == 0
     assert 0 < sas.workspace_size(cfg, sas.OP_ATTENTION_CHUNK, 4096, 1) < 70 << 20
 
@@ -174,3 +176,18 @@ def test_the_binding_refuses_host_tensors():
         sas.plan_chunk(None, i, i, i, i, i[:1], 4)
     with pytest.raises(sas.SasError, match="not a tensor on the GPU"):
         sas.verify_drafts(t[0].float(), None, i, i, i, i, 4)
+
+
+def test_the_binding_refuses_rows_that_overlap():
+    cfg, cpu = config(4, 2, 128), torch.device("cpu")
+    t = torch.zeros(1, 4, 128, dtype=torch.bfloat16)
+    for x in (t.expand(5, 4, 128), torch.zeros(2048, dtype=torch.bfloat16).as_strided((5, 4, 128), (256, 128, 1))):
+        with pytest.raises(sas.SasError, match="do not overlap"):
+            sas._heads_arg(cfg, "q", x, 4, 5, cpu)
+    assert sas._heads_arg(cfg, "q", t, 4, 1, cpu)[1] == 512
+
+
+@pytest.mark.parametrize("n,least", [(-1, 0), (0, 1), (2 ** 31, 0), (2 ** 32 + 5, 1)])
+def test_counts_fit_the_arguments(n, least):
+    with pytest.raises(sas.SasError, match="from"):
+        sas._count("rows", n, least)
