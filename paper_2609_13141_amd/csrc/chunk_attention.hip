@@ -252,9 +252,10 @@ __device__ __forceinline__ ChunkJob chunk_wave_plan(const ChunkArgs& P, int keys
   return out;
 }
 
-// The pages of a sequence, as a wave holds them: lane l has the page of the tile's key l
-// (-1: no such key, or unmapped), and then the byte offset of that key's row of kv head g
-// in the pools (page 0 for keys without one).
+// The pages of a sequence, as a wave holds them: lane l has the block-table entry of the
+// tile's key l (`load`; looked at only a tile later, because a look would wait for all
+// loads in flight), its page (-1: no such key, or unmapped), and then the byte offset of
+// that key's row of kv head g in the pools (page 0 for keys without one).
 template <typename T, int DH>
 struct ChunkPages {
   const ChunkArgs& P;
@@ -262,9 +263,10 @@ struct ChunkPages {
   int g, keys, lane;
   static constexpr int KEYS = ChunkTile<T>::KEYS, RB = DH * (int)sizeof(T);
   __device__ __forceinline__ int load(int kt) const {
-    const int p = kt * KEYS + (lane & (KEYS - 1));
-    const int page = row[min(p >> P.ps_shift, P.max_pages - 1)];
-    return p < keys && page >= 0 && page < P.num_pages ? page : -1;
+    return row[min((kt * KEYS + (lane & (KEYS - 1))) >> P.ps_shift, P.max_pages - 1)];
+  }
+  __device__ __forceinline__ int page(int kt, int entry) const {
+    return kt * KEYS + (lane & (KEYS - 1)) < keys && entry >= 0 && entry < P.num_pages ? entry : -1;
   }
   __device__ __forceinline__ uint64_t offset(int kt, int page) const {
     const uint32_t stride = ((uint32_t)P.Hkv << P.ps_shift) * RB;  // bytes of a page
@@ -276,34 +278,56 @@ struct ChunkPages {
   }
 };
 
+// 16 bytes a lane from `at` past `rows` and the constant `from`, to LDS at d + from
+template <int from, typename Rows>
+__device__ __forceinline__ void chunk_copy_piece(const Rows& rows, chunk_lds_t* d, uint32_t at) {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass does not know 16-byte pieces)
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, d, 16, at, 0, from, 0);
+#endif
+}
+
+// A buffer of n bytes, `off` past `pool` (0x27000: plain 32-bit elements, no swizzle)
+__device__ __forceinline__ auto chunk_rows(const void* pool, uint64_t off, int n) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)pool + off), 0, n, 0x27000);
+}
+
 // Copies a tile's rows from `pool` straight to LDS (256 threads), given the keys' row
 // offsets.  A wave copies KEYS / 4 consecutive rows, NL pieces of 1 KB in both places:
 // where the rows share a page, one scalar address serves them all (the instruction's
 // offset moves both sides) and the lanes' own offsets are those of every tile, so that
-// the copy takes next to nothing of either unit.
+// the copy takes next to nothing of either unit; in smaller pages each piece has its
+// own.  Those are buffer loads: while loads from the lanes' own addresses are in flight,
+// the compiler lets every LDS read wait for all LDS reads before it.  Pages smaller than
+// a piece's rows need such loads, which are waited for here for that reason.
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_copy(const ChunkArgs& P, const void* pool, unsigned char* dst, uint64_t off, int wave,
                                            int lane) {
   constexpr int KEYS = ChunkTile<T>::KEYS, RB = DH * (int)sizeof(T), CH = RB / 16, NL = KEYS * CH / 256, RW = 64 / CH;
+  static_assert(NL == 2 || NL == 4, "pieces");
   const int lo = (int)(uint32_t)off, hi = (int)(uint32_t)(off >> 32);
   asm volatile("" : "+v"(lane));  // (formed anew per tile: kept, the offsets would spill)
   chunk_lds_t* const d = (chunk_lds_t*)(dst + wave * NL * 1024);
-  if ((1 << P.ps_shift) >= KEYS / 4) {
-    const int r0 = wave * (KEYS / 4);
-    uint64_t base = (uint64_t)pool + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(lo, r0) |
-                                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, r0) << 32);
-    asm("" : "+s"(base));  // (kept apart from the lanes' offsets: summed, they would be vector arithmetic)
+  const int r0 = wave * (KEYS / 4);
+  if ((1 << P.ps_shift) >= RW) {
     // (the swizzle permutes bits of the row, and the pieces' first rows share none with lane / CH)
     const uint32_t first = lane / CH * RB + (((lane % CH) ^ chunk_swz<T, DH>(lane / CH) ^ chunk_swz<T, DH>(r0)) << 4);
-#define CHUNK_PIECE(i)                                                                                         \
-  if constexpr (i < NL) {                                                                                      \
-    uint32_t at = first ^ (chunk_swz<T, DH>(i * RW) << 4);                                                     \
-    asm("" : "+v"(at));                                                                                        \
-    __builtin_amdgcn_global_load_lds((const void*)(base + at), d, 16, i * 1024, 0);                            \
-  }
-    CHUNK_PIECE(0) CHUNK_PIECE(1) CHUNK_PIECE(2) CHUNK_PIECE(3)
-#undef CHUNK_PIECE
-    static_assert(NL <= 4, "pieces");
+    auto at = [&](int i) { return first ^ (chunk_swz<T, DH>(i * RW) << 4); };
+    auto lane_offset = [&](int r) {
+      return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(lo, r) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, r) << 32;
+    };
+    if ((1 << P.ps_shift) >= KEYS / 4) {
+      const auto rows = chunk_rows(pool, lane_offset(r0), NL * 1024);
+      chunk_copy_piece<0>(rows, d, at(0));
+      chunk_copy_piece<1024>(rows, d, at(1));
+      if constexpr (NL > 2) {
+        chunk_copy_piece<2048>(rows, d, at(2));
+        chunk_copy_piece<3072>(rows, d, at(3));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        chunk_copy_piece<0>(chunk_rows(pool, lane_offset(r0 + i * RW), 1024), (chunk_lds_t*)(dst + (wave * NL + i) * 1024), at(i));
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
@@ -312,6 +336,7 @@ __device__ __forceinline__ void chunk_copy(const ChunkArgs& P, const void* pool,
       __builtin_amdgcn_global_load_lds((const void*)((const char*)pool + at + c * 16),
                                        (chunk_lds_t*)(dst + (wave * NL + i) * 1024), 16, 0, 0);
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
   }
 }
 
@@ -439,6 +464,13 @@ __device__ __forceinline__ void chunk_store(const ChunkArgs& P, const ChunkSeq& 
   if (P.lse && lk == 0) P.lse[R.at] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
 }
 
+// The transposing LDS read of 8 bytes.  Without the qualifier the compiler would let each
+// wait for every direct-to-LDS load in flight, the next tiles' among them; what a tile
+// reads has been waited for at its barrier.
+__device__ __forceinline__ uint2 chunk_read_tr(lds_s16x4_t* __restrict p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(p));
+}
+
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   constexpr bool BF = sizeof(T) == 2;
@@ -503,7 +535,7 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   int pg = -1;
   unsigned long long vcur = 0;
   if (kt < tend) {
-    pg = pages.load(kt);
+    pg = pages.page(kt, pages.load(kt));
     load_tile(kt, pg, 0);
     vcur = pages.mapped(pg);
     pg = pages.load(kt + 1);
@@ -515,9 +547,10 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
     const int k0 = kt * KEYS;
     unsigned char* const tb = tiles + buf * 2 * TB;
     asm volatile("" : "+v"(o_row), "+v"(o_tr[0]), "+v"(o_tr[1]));  // (formed anew per tile: kept, they would spill)
-    const unsigned long long vnext = pages.mapped(pg);
+    const int pn = pages.page(kt + 1, pg);
+    const unsigned long long vnext = pages.mapped(pn);
     if (kt + 1 < tend) {
-      load_tile(kt + 1, pg, buf ^ 1);
+      load_tile(kt + 1, pn, buf ^ 1);
       pg = pages.load(kt + 2);
     }
     const bool diag = k0 + KEYS - 1 > t0, gaps = vcur != ALL;
@@ -626,8 +659,8 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
           const bf16x8_t pb = *(const bf16x8_t*)&pu;
 #pragma unroll
           for (int dt = 0; dt < DH / 32; ++dt) {
-            const uint2 lo = lds_read_tr(tb + TB + (o_tr[0] ^ (dt << 6)) + ks * 16 * RB);
-            const uint2 hi = lds_read_tr(tb + TB + (o_tr[1] ^ (dt << 6)) + ks * 16 * RB);
+            const uint2 lo = chunk_read_tr((lds_s16x4_t*)(tb + TB + (o_tr[0] ^ (dt << 6)) + ks * 16 * RB));
+            const uint2 hi = chunk_read_tr((lds_s16x4_t*)(tb + TB + (o_tr[1] ^ (dt << 6)) + ks * 16 * RB));
             const uint4 vu = make_uint4(lo.x, lo.y, hi.x, hi.y);
             o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t*)&vu, pb, o[dt], 0, 0, 0);
           }
@@ -653,12 +686,9 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
   chunk_store<T, DH>(P, S, tile, g, rel, sp, o, m_run, l_run, wave, lane);
 }
 
-// LDS reads at a 32-bit address: 16 bytes, and the transposing read of 8
+// LDS read of 16 bytes at a 32-bit address
 __device__ __forceinline__ bf16x8_t lds_read16(uint32_t a) {
   return *(const __attribute__((address_space(3))) bf16x8_t*)(uintptr_t)a;
-}
-__device__ __forceinline__ uint2 lds_read_tr(uint32_t a) {
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)a));
 }
 
 // the larger of x in lanes l and l ^ 32
@@ -708,9 +738,47 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
     for (int v = 0; v < 16; ++v) o[dt][v] = 0.f;
   const float qk_scale = P.sm_scale * LOG2E;
 
-  const ChunkPages<T, DH> pages = {P, P.table + (size_t)seq * P.max_pages, g, S.keys, lane};
-  auto load_k = [&](int kt, uint64_t off) { chunk_copy<T, DH>(P, P.k_pages, tiles + ((kt - tlo) & 1) * TB, off, wave, lane); };
-  auto load_v = [&](int kt, uint64_t off) { chunk_copy<T, DH>(P, P.v_pages, tiles + (2 + ((kt - tlo) & 1)) * TB, off, wave, lane); };
+  // Pages: lane j of every four has the block-table entry of the tile's j-th 16 keys (a
+  // page has at least as many), looked at a tile later, because a look waits for all loads
+  // in flight; the rest is scalar.  A wave copies 16 keys' rows, in pieces of 1 KB.
+  constexpr int NL = RB / 64, CH = RB / 16, RW = 64 / CH;
+  const int32_t* const table = P.table + (size_t)seq * P.max_pages;
+  const int key0 = (lane & 3) * 16;
+  auto entries = [&](int kt) { return table[min((kt * KEYS + key0) >> P.ps_shift, P.max_pages - 1)]; };
+  struct Pages {
+    unsigned long long vm;  // keys with a page
+    uint64_t off;           // offset of this wave's first row in the pools (in page 0 without one)
+  };
+  auto look = [&](int kt, int entry) {
+    const bool ok = entry >= 0 && entry < P.num_pages && kt * KEYS + key0 < S.keys;
+    const uint32_t m4 = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
+    const uint32_t page = m4 >> wave & 1 ? (uint32_t)__builtin_amdgcn_readlane(entry, wave) : 0;
+    const uint32_t in = ((uint32_t)g << P.ps_shift) + ((kt * KEYS + wave * 16) & ((1 << P.ps_shift) - 1));
+    const int left = S.keys - kt * KEYS;
+    Pages r = {~0ull, (uint64_t)page * (((uint32_t)P.Hkv << P.ps_shift) * RB) + in * RB};
+    if ((m4 & 15) != 15 || left < KEYS) {
+      r.vm = 0;
+      for (int j = 0; j < 4; ++j) r.vm |= m4 >> j & 1 ? 0xffffull << (16 * j) : 0;
+      if (left < KEYS) r.vm &= (1ull << max(left, 0)) - 1;
+    }
+    return r;
+  };
+  uint32_t at[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i)
+    at[i] = lane / CH * RB + (((lane % CH) ^ chunk_swz<T, DH>(wave * 16 + i * RW + lane / CH)) << 4);
+  auto copy = [&](const void* pool, unsigned char* dst, uint64_t off) __attribute__((always_inline)) {
+    const auto rows = chunk_rows(pool, off, NL * 1024);
+    chunk_lds_t* const d = (chunk_lds_t*)(dst + wave * NL * 1024);
+    chunk_copy_piece<0>(rows, d, at[0]);
+    chunk_copy_piece<1024>(rows, d, at[1]);
+    if constexpr (NL > 2) {
+      chunk_copy_piece<2048>(rows, d, at[2]);
+      chunk_copy_piece<3072>(rows, d, at[3]);
+    }
+  };
+  auto load_k = [&](int kt, uint64_t off) { copy(P.k_pages, tiles + ((kt - tlo) & 1) * TB, off); };
+  auto load_v = [&](int kt, uint64_t off) { copy(P.v_pages, tiles + (2 + ((kt - tlo) & 1)) * TB, off); };
   auto tile_barrier = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(chunk_lds_t*)tiles;  // aligned to a row
@@ -766,21 +834,21 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
     }
   };
   unsigned long long vm = 0, vm1 = 0;  // keys of tiles kt and kt + 1 with a page
-  uint64_t off1 = 0;                   // row offsets of tile kt + 1
-  int pg2 = -1;                        // pages of tile kt + 2
+  uint64_t off1 = 0;                   // where tile kt + 1 is
+  int e2 = -1;                         // block-table entries of tile kt + 2
   auto special = [&](int kt, unsigned long long v) { return kt * KEYS + KEYS - 1 > t0 || v != ~0ull; };
   if (tlo < tend) {
     floatx16_t s0, s1, u0, u1;  // (a tile's halves, by turns)
     {
-      const int pg0 = pages.load(tlo), pg1 = pages.load(tlo + 1);
-      const uint64_t off0 = pages.offset(tlo, pg0);
-      off1 = pages.offset(tlo + 1, pg1);
-      load_k(tlo, off0);
-      load_v(tlo, off0);
-      if (tlo + 1 < tend) load_k(tlo + 1, off1);
-      pg2 = pages.load(tlo + 2);
-      vm = pages.mapped(pg0);
-      vm1 = pages.mapped(pg1);
+      const int e0 = entries(tlo), e1 = entries(tlo + 1);
+      const Pages p0 = look(tlo, e0), p1 = look(tlo + 1, e1);
+      load_k(tlo, p0.off);
+      load_v(tlo, p0.off);
+      if (tlo + 1 < tend) load_k(tlo + 1, p1.off);
+      e2 = entries(tlo + 2);
+      vm = p0.vm;
+      vm1 = p1.vm;
+      off1 = p1.off;
     }
     float mx;
     tile_barrier();
@@ -795,12 +863,11 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
     auto tile = [&](int kt, floatx16_t& s0, floatx16_t& s1, floatx16_t& n0, floatx16_t& n1, auto odd_t) __attribute__((always_inline)) {
       constexpr int odd = decltype(odd_t)::value;
       tile_barrier();  // K(kt + 1) and V(kt) are there; K(kt) and V(kt - 1) are free
-      const unsigned long long vm2 = pages.mapped(pg2);
-      const uint64_t off2 = pages.offset(kt + 2, pg2);
+      const Pages p2 = look(kt + 2, e2);
       if (kt + 1 < tend) load_v(kt + 1, off1);
-      if (kt + 2 < tend) load_k(kt + 2, off2);
-      off1 = off2;
-      pg2 = pages.load(kt + 3);
+      if (kt + 2 < tend) load_k(kt + 2, p2.off);
+      off1 = p2.off;
+      e2 = entries(kt + 3);
       const bool masked = special(kt, vm), masked1 = special(kt + 1, vm1);
       if (masked) chunk_fix_values<T, DH>(tiles + (2 + odd) * TB, &bad_s, kt * KEYS, vm, t, o, wave, lane);
       constexpr uint32_t kb = (odd ^ 1) * TB, vb = (2 + odd) * TB;
@@ -818,8 +885,8 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
         const float bias = m_run == -INFINITY ? 0.f : -m_run;
         auto read_k = [&](int ks) { kf[ks] = lds_read16((o_row ^ (ks << 5)) + kb + st * 32 * RB); };
         auto read_v = [&](uint4* f, int dt, int ks) {
-          const uint2 lo = lds_read_tr((o_tr[0] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB);
-          const uint2 hi = lds_read_tr((o_tr[1] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB);
+          const uint2 lo = chunk_read_tr((lds_s16x4_t*)(uintptr_t)((o_tr[0] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB));
+          const uint2 hi = chunk_read_tr((lds_s16x4_t*)(uintptr_t)((o_tr[1] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB));
           f[dt] = make_uint4(lo.x, lo.y, hi.x, hi.y);
         };
         // P is rounded to bf16 for the matrix instruction; the sum keeps the fp32 weights
@@ -879,7 +946,7 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
       }
       if (kt + 1 < tend) reference(mx);
       vm = vm1;
-      vm1 = vm2;
+      vm1 = p2.vm;
     };
     for (int kt = tlo;;) {
       tile(kt, s0, s1, u0, u1, std::integral_constant<int, 0>{});
@@ -1053,7 +1120,7 @@ hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) 
   const int least = dtype == SAS_BF16 ? ChunkTile<bf16_t>::LEAST : ChunkTile<float>::LEAST;
   // the pipelined kernel where the average sequence fills a tile: with fewer rows the
   // keys' bytes bound the call
-  const bool piped = dtype == SAS_BF16 && (long long)a.rows * G > (long long)CHUNK_ROWS * std::min(a.b, a.rows);
+  const bool piped = dtype == SAS_BF16 && a.ps_shift >= 4 && (long long)a.rows * G > (long long)CHUNK_ROWS * std::min(a.b, a.rows);
   // (tile, kv head) pairs, at most
   const long long tiles = ((long long)a.rows / (CHUNK_ROWS / G) + std::min(a.b, a.rows)) * a.Hkv;
   ChunkKernels k;

@@ -62,7 +62,7 @@ def test_captured_replays_of_the_job_queues():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("ps,new", [(16, 3), (16, 90), (2, 3)])
+@pytest.mark.parametrize("ps,new", [(16, 3), (16, 90), (8, 40), (4, 3), (4, 90), (2, 3), (2, 90)])
 def test_pools_past_4_gib(dtype, ps, new):
     """The same pages at the two ends of a pool larger than 2^32 bytes: the same bits."""
     H, Hkv, dh, B = 16, 16, 128, 64
