@@ -697,17 +697,19 @@ __device__ __forceinline__ float pair_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// The same job (bf16), pipelined inside the wave for calls that the matrix unit bounds:
-// 32 keys at a time, the matrix unit forms the scores of the next tile while the vector
-// unit takes this tile's exponentials and sums, and adds the products with the values
-// while it takes the maxima of the following scores; none waits for the other.  K runs a
-// tile ahead of V in LDS: an iteration reads K(t + 1) and V(t) and loads K(t + 2) and
-// V(t + 1), with one barrier.  2048 tokens over 30005 cached, 28/4 heads of 128: 0.95 ms
-// (0.96 PFLOP/s; the plain loop 1.04, a large product reaches 1.4 PFLOP/s).  The vector
-// unit bounds it: about 230 instructions a wave and tile, 32 of them exponentials, against
-// 32 products of 32 cycles; addresses kept in registers instead of formed for each tile
-// took 2% off.  Not kept: 64 keys at a time (181 spilled registers, 3.1 ms), 64 rows a
-// wave with the fragments shared (340).
+// The same job (bf16, pages of 16 keys or more), pipelined inside the wave for calls that
+// the matrix unit bounds: 32 keys at a time, the matrix unit forms the scores of the next
+// tile while the vector unit takes this tile's exponentials and sums, then the products
+// with the values; none waits for the other.  K runs a tile ahead of V in LDS: an
+// iteration reads K(t + 1) and V(t) and loads K(t + 2) and V(t + 1), with one barrier.
+// 2048 tokens over 30005 cached, 28/4 heads of 128: 0.885 ms (1.03 PFLOP/s; the plain
+// loop 0.961 ms, a large product reaches 1.4 PFLOP/s); 2304 tokens, whose tiles fill every
+// workgroup, 1.08 PFLOP/s.  What bounds it is the card's power: the clock is at 1.9 GHz
+// of 2.4 (1.8 in a loop of nothing but products), and removing waits alone, 2% of the
+// cycles, took no time off; removing vector instructions did: page lookups in scalar
+// registers (15% of them) 2%, no maxima but where the reference moves 6%.  Not kept: 64
+// keys at a time (181 spilled registers, 3.1 ms), 64 rows a wave with the fragments
+// shared (340).
 template <int DH>
 __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   using T = bf16_t;
@@ -810,22 +812,20 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
       if (kt * KEYS + j + lk4 > t || !((vm >> j) & 1)) s[v] = -INFINITY;
     }
   };
-  // row maximum of the scaled logits (the scale is positive)
-  auto maximum = [&](const floatx16_t& s) __attribute__((always_inline)) {
-    float m = s[0];
+  // The reference of the exponentials.  Any gives the same sums, so it is looked at only
+  // where a lane's 16 weights add up to more than `limit`: one of them then exceeds 2^8
+  // (or is the first of its row), and the reference moves to the row's maximum.
+  float limit = 0.f;
+  auto reference = [&](const floatx16_t& s) __attribute__((always_inline)) {
+    float mx = s[0];
 #pragma unroll
-    for (int v = 1; v < 16; ++v) m = fmaxf(m, s[v]);
-    return pair_max(m * qk_scale);
-  };
-  // The reference moves only where a logit exceeds it by more than 8, in log2 units (any
-  // reference gives the same sums); what is summed so far is then rescaled.
-  auto reference = [&](float mx) __attribute__((always_inline)) {
-    const bool move = mx > m_run + 8.f;
-    if (__builtin_amdgcn_ballot_w64(move) == 0) return;
-    if (move) {
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
+    mx = pair_max(mx * qk_scale);  // (the scale is positive)
+    if (mx > m_run + 8.f) {
       // (nothing is summed yet where m_run is -inf)
       const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mx);
       m_run = mx;
+      limit = 4096.f;
       l_run *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt)
@@ -850,14 +850,12 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
       vm1 = p1.vm;
       off1 = p1.off;
     }
-    float mx;
     tile_barrier();
     // both halves of K(tlo) are read before the first iteration's loads replace it
     product(s0, 0, 0);
     product(s1, 0, 1);
     if (special(tlo, vm)) mask(s0, tlo, 0, vm);
-    mx = maximum(s0);
-    reference(mx);
+    reference(s0);
     // tile kt, of scores s0 and s1; leaves those of the next in n0 and n1
     // (odd: the tile lies in the odd buffers, counted from tlo)
     auto tile = [&](int kt, floatx16_t& s0, floatx16_t& s1, floatx16_t& n0, floatx16_t& n1, auto odd_t) __attribute__((always_inline)) {
@@ -871,18 +869,17 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
       const bool masked = special(kt, vm), masked1 = special(kt + 1, vm1);
       if (masked) chunk_fix_values<T, DH>(tiles + (2 + odd) * TB, &bad_s, kt * KEYS, vm, t, o, wave, lane);
       constexpr uint32_t kb = (odd ^ 1) * TB, vb = (2 + odd) * TB;
-      // Half st of the tile, whose scores s turn into those of the next tile's half: the
-      // products of those between this half's exponentials and sums, then its products
-      // with the values between the maxima of the following half, `after`.  One product
-      // takes the matrix unit 32 cycles, about what a step's vector instructions take the
-      // other; the steps are pinned, because the compiler groups each kind of instruction.
-      auto half = [&](const floatx16_t& s, floatx16_t& n, const floatx16_t& after, int st) __attribute__((always_inline)) {
+      // Half st of the tile, of scores s; leaves the next tile's in n: their products
+      // between this half's exponentials and sums, then its products with the values.  One
+      // product takes the matrix unit 32 cycles, more than a step's vector instructions take
+      // the other; the steps are pinned, because the compiler groups each kind of instruction.
+      auto half = [&](const floatx16_t& s, floatx16_t& n, int st) __attribute__((always_inline)) {
         constexpr int NK = DH / 16, ND = DH / 32, PER = 16 / NK;  // steps, groups of dimensions, weights a step
         uint32_t pk[8];
         uint4 f0[ND], f1[ND];
         bf16x8_t kf[NK];
         float p[16], r2[2] = {0.f, 0.f};
-        const float bias = m_run == -INFINITY ? 0.f : -m_run;
+        float bias = m_run == -INFINITY ? 0.f : -m_run;
         auto read_k = [&](int ks) { kf[ks] = lds_read16((o_row ^ (ks << 5)) + kb + st * 32 * RB); };
         auto read_v = [&](uint4* f, int dt, int ks) {
           const uint2 lo = chunk_read_tr((lds_s16x4_t*)(uintptr_t)((o_tr[0] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB));
@@ -918,8 +915,16 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
 #pragma unroll
         for (int dt = 3; dt < ND; ++dt) read_v(f0, dt, 0);
         __builtin_amdgcn_sched_barrier(0);
+        if (__builtin_amdgcn_ballot_w64(!(r2[0] + r2[1] <= limit)) != 0) {
+          reference(s);
+          bias = m_run == -INFINITY ? 0.f : -m_run;
+          r2[0] = r2[1] = 0.f;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) p[v] = __builtin_amdgcn_exp2f(fmaf(s[v], qk_scale, bias));
+#pragma unroll
+          for (int u = 0; u < NK; ++u) finish(u);
+        }
         l_run += r2[0] + r2[1];  // this lane's keys
-        float m = after[0];
 #pragma unroll
         for (int u = 0; u < 2 * ND; ++u) {
           const int dt = u % ND, v0 = 4 * (u / ND);
@@ -927,24 +932,13 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
           const uint4 pu = make_uint4(pk[v0], pk[v0 + 1], pk[v0 + 2], pk[v0 + 3]);
           const uint4& f = u < ND ? f0[dt] : f1[dt];
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t*)&f, *(const bf16x8_t*)&pu, o[dt], 0, 0, 0);
-#pragma unroll
-          for (int v = u * PER; v < (u + 1) * PER; ++v) m = fmaxf(m, after[v]);
           __builtin_amdgcn_sched_barrier(0);
         }
-        mx = pair_max(m * qk_scale);
       };
-      half(s0, n0, s1, 0);
-      if (masked) {
-        mask(s1, kt, 1, vm);
-        mx = maximum(s1);
-      }
-      reference(mx);
-      half(s1, n1, n0, 1);
-      if (masked1) {
-        mask(n0, kt + 1, 0, vm1);
-        mx = maximum(n0);
-      }
-      if (kt + 1 < tend) reference(mx);
+      half(s0, n0, 0);
+      if (masked) mask(s1, kt, 1, vm);
+      half(s1, n1, 1);
+      if (masked1) mask(n0, kt + 1, 0, vm1);
       vm = vm1;
       vm1 = p2.vm;
     };
@@ -1119,7 +1113,9 @@ hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) 
   const int keys = dtype == SAS_BF16 ? ChunkTile<bf16_t>::KEYS : ChunkTile<float>::KEYS;
   const int least = dtype == SAS_BF16 ? ChunkTile<bf16_t>::LEAST : ChunkTile<float>::LEAST;
   // the pipelined kernel where the average sequence fills a tile: with fewer rows the
-  // keys' bytes bound the call
+  // keys' bytes bound the call (by it and by the plain loop: 2048 new tokens of 32/32
+  // heads 79.2 and 86.4 us, 4 x 512 of 28/4 heads 32.1 and 33.7; 8 x 1 over 2300 of 32/32
+  // heads 60.7 and 57.4, 32 x 5 over 4000 of 28/4 55.9 and 54.1)
   const bool piped = dtype == SAS_BF16 && a.ps_shift >= 4 && (long long)a.rows * G > (long long)CHUNK_ROWS * std::min(a.b, a.rows);
   // (tile, kv head) pairs, at most
   const long long tiles = ((long long)a.rows / (CHUNK_ROWS / G) + std::min(a.b, a.rows)) * a.Hkv;

@@ -180,3 +180,20 @@ def test_two_captured_backwards_on_two_streams():
                 assert torch.equal(o[n], w[n]), n
             for a, b in zip(f, sas.qk_norm_rope(cfg, *s[:3], *s[5:])):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ramp", ["up", "down", "jump", "late"])
+def test_logits_that_grow_with_the_position(dtype, ramp):
+    """The running maximum moves on many tiles, on one by more than fp32 exponentials
+    reach, or never again."""
+    cfg = config(4, 2, 128, 64, dtype)
+    c = Chunk([700, 90], [200, 150], 4, 2, 128, 16, 64, dtype, seed=70)
+    p = torch.arange(900, device="cuda", dtype=torch.float32)
+    w = {"up": p / 60, "down": (900 - p) / 60, "jump": torch.where(p < 333, 0.01, 40.0),
+         "late": torch.where(p < 690, 0.0, 60.0)}[ramp].to(c.q.dtype)
+    for i, n in ((0, 900), (1, 240)):
+        at = torch.arange(n, device="cuda")
+        pg = c.cache.block_table[i, at // 16].long()
+        c.cache.k_pages[pg, :, at % 16] *= w[at][:, None, None]
+    check_attention(c, run(c, cfg), dtype)
