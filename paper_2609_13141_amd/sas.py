@@ -684,20 +684,15 @@ def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free
                 _need("pages_held", pages_held, i32, (b,), dev), _need("free_pages", free_pages, i32, (free_pages.numel(),), dev),
                 _need("free_count", free_count, i32, (1,), dev), _count("entries of free_pages", free_pages.numel()))
     # one allocation for the int32 outputs, each at a multiple of 16 bytes
-    sizes, names = [], []
-    for name, n in (("seq", rows), ("pos", rows), ("kv_len", b), ("pages_held", b), ("row_start", b + 1),
-                    ("free_count", 1), ("missing", 1)):
-        sizes.append(n)
-        names.append(name)
-        if n % 4:
-            sizes.append(-n % 4)
-            names.append(None)
-    out = dict(zip(names, torch.empty(sum(sizes), dtype=i32, device=dev).split_with_sizes(sizes)))
-    out.pop(None, None)
-    out["slot"] = torch.empty(rows, dtype=torch.int64, device=dev)
-    po = PlanOut(*[out[f].data_ptr() for f, _ in PlanOut._fields_])
+    sizes = (rows, -rows % 4, rows, -rows % 4, b, -b % 4, b, -b % 4, b + 1, -(b + 1) % 4, 1, 3, 1)
+    seq, _, pos, _, kv_len, _, held, _, start, _, count, _, missing = \
+        torch.empty(sum(sizes), dtype=i32, device=dev).split_with_sizes(sizes)
+    slot = torch.empty(rows, dtype=torch.int64, device=dev)
+    po = PlanOut(start.data_ptr(), kv_len.data_ptr(), seq.data_ptr(), pos.data_ptr(), slot.data_ptr(), held.data_ptr(),
+                 count.data_ptr(), missing.data_ptr())
     _call(dev, lib().sas_plan_chunk, b, rows, C.byref(pi), C.byref(kv), C.byref(po))
-    return out
+    return {"row_start": start, "kv_len": kv_len, "seq": seq, "pos": pos, "slot": slot, "pages_held": held,
+            "free_count": count, "missing": missing}
 
 
 def qk_norm_rope(cfg: Config, q, k, pos, gain_q=None, gain_k=None, *, sections=None):

@@ -197,3 +197,20 @@ def test_logits_that_grow_with_the_position(dtype, ramp):
         pg = c.cache.block_table[i, at // 16].long()
         c.cache.k_pages[pg, :, at % 16] *= w[at][:, None, None]
     check_attention(c, run(c, cfg), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh,ps", [(128, 16), (64, 16), (128, 32), (64, 64), (128, 128)])
+def test_long_chunks_over_pages_that_are_missing(dtype, dh, ps):
+    """Holes (entry -1, or no page of the pool) before and inside the chunk, at its
+    first and last page, a sequence without any page, and a block table that ends
+    before the last tokens' positions."""
+    B = max(ps, 64)
+    cfg = config(4, 2, dh, B, dtype)
+    n = 32 // (ps // 16)
+    unmap = [(0, 0), (0, n // 2, 10 ** 6), (0, n), (1, 1, -5), (1, 2)] + [(2, j) for j in range(60)]
+    c = Chunk([400, 100, 150, 333], [250, 170, 200, 205], 4, 2, dh, ps, B, dtype, seed=80, unmap=unmap, width=128)
+    check_attention(c, run(c, cfg), dtype)
+    short = -(-480 // ps)
+    c.cache.block_table = c.cache.block_table[:, :short].contiguous()
+    check_attention(c, run(c, cfg), dtype)
