@@ -1021,23 +1021,40 @@ __global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P, int res
 // 8 dimensions each.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(ChunkArgs P) {
-  if (P.head[1] == 0) return;
   constexpr int C8 = DH / 8, PG = 64 / C8;
   const int lane = threadIdx.x & 63, c8 = lane % C8, pg = lane / C8;
   const int G = P.H / P.Hkv, QPT = CHUNK_ROWS / G;
-  const int last = min(P.row_start[P.b], P.rows);
+  // up to 64 sequences: each in a lane, loaded together (one wait instead of four)
+  const bool few = P.b <= 64;
+  const int li = min(lane, P.b - 1);
+  const int start = P.row_start[li], end = P.row_start[few ? li + 1 : P.b];
+  const int2 parts = P.seq_parts[li];
+  const int first = __builtin_amdgcn_readlane(start, 0);
+  const int last = min(few ? __builtin_amdgcn_readlane(end, P.b - 1) : __builtin_amdgcn_readfirstlane(end), P.rows);
+  if (P.head[1] == 0) return;
   for (long long it = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); it < (long long)P.rows * P.H;
        it += (long long)gridDim.x * 4) {
     const int r = (int)(it / P.H), h = (int)(it % P.H), g = h / G;
-    if (r < P.row_start[0] || r >= last) continue;
-    const int i = __builtin_amdgcn_readfirstlane(wave_find(P.row_start, P.b, r, lane));
-    const int2 sp = P.seq_parts[i];
+    if (r < first || r >= last) continue;
+    int2 sp;
+    int r0, r1;
+    if (few) {
+      const int i = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(lane < P.b && start <= r));
+      sp = make_int2(__builtin_amdgcn_readlane(parts.x, i), __builtin_amdgcn_readlane(parts.y, i));
+      r0 = __builtin_amdgcn_readlane(start, i);
+      r1 = __builtin_amdgcn_readlane(end, i);
+    } else {
+      const int i = __builtin_amdgcn_readfirstlane(wave_find(P.row_start, P.b, r, lane));
+      sp = P.seq_parts[i];
+      r0 = P.row_start[i];
+      r1 = P.row_start[i + 1];
+    }
     if (sp.x <= 1) continue;
-    const ChunkSeq S = chunk_seq(P, i);
-    const int j = r - S.r0;
-    if (j >= S.m) continue;
-    const int ntile = (S.m + QPT - 1) / QPT, tile = j / QPT, pl = j - tile * QPT;
-    const int R = min(S.m, QPT) * G;  // rows of a part
+    r0 = min(max(r0, 0), P.rows);  // (as chunk_seq)
+    const int m = min(max(r1, r0), P.rows) - r0, j = r - r0;
+    if (j >= m) continue;
+    const int ntile = (m + QPT - 1) / QPT, tile = j / QPT, pl = j - tile * QPT;
+    const int R = min(m, QPT) * G;  // rows of a part
     const size_t s0 = (size_t)sp.y + (size_t)(g * ntile + (ntile - 1 - tile)) * sp.x * R + pl * G + (h - g * G);
     const float2* ml = (const float2*)P.part_ml + s0;
     float mx = -INFINITY;
