@@ -8,11 +8,12 @@
 //
 // Only one row of p and one of q are read in full, b vocab (4 or 8) bytes.  The
 // vocabulary is cut in sixteen, the sixteenth that the uniform falls into in sixteen
-// again, until a wave can scan it token by token.  A workgroup a sequence does it all
+// again, until a wave can scan it token by token (eight a lane, loaded together; 64 at a
+// time 2.4 us more of 29, all waves scanning another 1).  A workgroup a sequence does it all
 // up to VERIFY_ONE tokens; one compute unit reads some 21 GB/s, so that the sums of
 // larger vocabularies are taken by sixteen workgroups a sequence first:
-//   8 x  32000: one workgroup 12 us, two kernels 4 + 11;
-//   128 x 100003 (102 MB): one workgroup 46 us, two kernels 18 + 11.
+//   8 x  32000: one workgroup 11.5 us, two kernels 4 + 11;
+//   128 x 100003 (102 MB): one workgroup 46 us, two kernels 18 + 7.
 // Differences and sums are fp64: the fp32 inputs' products and differences are exact
 // there, and a token's border in the CDF is some 1e-16 wide rather than the 1e-7 of an
 // fp32 sum.
@@ -22,6 +23,7 @@
 namespace sas {
 
 constexpr int VERIFY_WAVES = 16;  // and pieces of a cut
+constexpr int VERIFY_LANE = 8;    // tokens of a lane in the last one
 
 // tokens of a piece of n, whole steps of a wave
 __host__ __device__ __forceinline__ int verify_piece(int n) { return ((n + VERIFY_WAVES - 1) / VERIFY_WAVES + 63) / 64 * 64; }
@@ -170,7 +172,7 @@ __global__ void __launch_bounds__(VERIFY_WAVES * 64) verify_kernel(VerifyArgs P)
       before = at;
       e0 += pick * len;
       e1 = min(e0 + len, e1);
-      if (e1 - e0 <= 512) break;
+      if (e1 - e0 <= 64 * VERIFY_LANE) break;
       const int whole = len;
       len = verify_piece(known ? whole : e1 - e0);
       if (known) {
@@ -182,28 +184,50 @@ __global__ void __launch_bounds__(VERIFY_WAVES * 64) verify_kernel(VerifyArgs P)
         verify_sums(v, e0, e1, len, s);
       }
     }
-    // token by token, 64 at a time
-    for (int b0 = e0; b0 < e1; b0 += 64) {
-      const int e = b0 + lane;
-      const double w = e < e1 ? verify_weight(v, e) : 0.0;
-      double x = w;
+    if (tid >= 64) return;  // (the others have no more to do)
+    // token by token, a lane eight of them
+    const int b0 = e0 + lane * VERIFY_LANE;
+    float p[VERIFY_LANE], q[VERIFY_LANE];
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(x, o, 64);
-        if (lane >= o) x += y;
-      }
-      const unsigned long long any = __builtin_amdgcn_ballot_w64(w > 0.0);
-      const unsigned long long hit = __builtin_amdgcn_ballot_w64(w > 0.0 && before + x > aim);
-      if (any) token = b0 + 63 - __builtin_clzll(any);
-      if (hit) {
-        token = b0 + __builtin_ctzll(hit);
-        break;
-      }
-      before += __shfl(x, 63, 64);
+    for (int u = 0; u < VERIFY_LANE; ++u) p[u] = v.p[min(b0 + u, e1 - 1)];
+#pragma unroll
+    for (int u = 0; u < VERIFY_LANE; ++u) q[u] = 0.f;
+    if (v.q) {
+#pragma unroll
+      for (int u = 0; u < VERIFY_LANE; ++u) q[u] = v.q[min(b0 + u, e1 - 1)];
     }
+    double w[VERIFY_LANE], sum = 0.0;
+#pragma unroll
+    for (int u = 0; u < VERIFY_LANE; ++u) {
+      const double d = (double)p[u] - (double)q[u];
+      w[u] = b0 + u < e1 && b0 + u != v.skip && d > 0.0 ? d : 0.0;
+      sum += w[u];
+    }
+    double x = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(x, o, 64);
+      if (lane >= o) x += y;
+    }
+    double to = __shfl_up(x, 1, 64);  // the sum before this lane's tokens, and then of them
+    to = lane ? before + to : before;
+    int hit = -1, some = -1;  // the first token past the aim, the last of any weight
+#pragma unroll
+    for (int u = 0; u < VERIFY_LANE; ++u) {
+      to += w[u];
+      if (w[u] > 0.0) {
+        some = b0 + u;
+        if (hit < 0 && to > aim) hit = b0 + u;
+      }
+    }
+    const unsigned long long hits = __builtin_amdgcn_ballot_w64(hit >= 0);
+    const unsigned long long any = __builtin_amdgcn_ballot_w64(some >= 0);
+    if (hits) token = __shfl(hit, __builtin_ctzll(hits), 64);
+    else if (any) token = __shfl(some, 63 - __builtin_clzll(any), 64);
   }
+  if (tid >= 64) return;
   const int W = P.max_draft + 1;
-  for (int j = tid; j < W; j += VERIFY_WAVES * 64)
+  for (int j = lane; j < W; j += 64)
     P.out[(size_t)i * W + j] = j < v.acc ? P.tokens[v.r0 + j] : j == v.acc ? token : -1;
   if (tid == 0) P.accepted[i] = v.acc;
 }
