@@ -457,10 +457,11 @@ struct VerifyArgs {
   const int32_t *tokens, *start;   // [rows], [b + 1]
   const float *u_accept, *u_sample;
   int32_t *out, *accepted;         // [b, max_draft + 1], [b]
-  double* part;                    // [b, 16, 16] sums of pieces (vocab > VERIFY_ONE)
+  double* part;                    // [b, 16, 16] sums of pieces, where verify_one does not hold
 };
-constexpr int VERIFY_ONE = 32768;  // the largest vocabulary of a single workgroup
-inline size_t verify_scratch_bytes(int b, int vocab) { return vocab > VERIFY_ONE ? (size_t)b * 256 * sizeof(double) : 0; }
+// Whether a workgroup a sequence does it all.
+inline bool verify_one(int b, int vocab) { return vocab <= 65536 || b >= 128; }
+inline size_t verify_scratch_bytes(int b, int vocab) { return verify_one(b, vocab) ? 0 : (size_t)b * 256 * sizeof(double); }
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s);
 
 // ---- model_ends.hip --------------------------------------------------------

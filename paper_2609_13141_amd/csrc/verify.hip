@@ -9,14 +9,16 @@
 // Only one row of p and one of q are read in full, b vocab (4 or 8) bytes.  The
 // vocabulary is cut in sixteen, the sixteenth that the uniform falls into in sixteen
 // again, until a wave can scan it token by token (eight a lane, loaded together; 64 at a
-// time 2.4 us more of 29, all waves scanning another 1).  A workgroup a sequence does it all
-// up to VERIFY_ONE tokens; one compute unit reads some 21 GB/s, so that the sums of
-// larger vocabularies are taken by sixteen workgroups a sequence first:
-//   8 x  32000: one workgroup 11.5 us, two kernels 4 + 11;
-//   128 x 100003 (102 MB): one workgroup 46 us, two kernels 18 + 7.
+// time 2.4 us more of 29, all waves scanning another 1).  A workgroup a sequence does it
+// all; where few sequences have large vocabularies, sixteen take a sequence's sums first
+// (captured, one workgroup and two kernels):
+//   8 x 32000: 10.2 and 11.7 us, 8 x 65536: 12.7 and 13.0, 8 x 100003: 16.7 and 15.1;
+//   128 x 50000: 17.1 and 20.6, 128 x 100003 (102 MB): 25.3 and 26.4.
 // Differences and sums are fp64: the fp32 inputs' products and differences are exact
 // there, and a token's border in the CDF is some 1e-16 wide rather than the 1e-7 of an
 // fp32 sum.
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -85,14 +87,25 @@ __device__ __forceinline__ double wave_sum_f64(double x) {
 __device__ __forceinline__ double verify_sum(const VerifyRow& v, int a, int b) {
   double w[4] = {0.0, 0.0, 0.0, 0.0};
   int e = a + (threadIdx.x & 63);
-  // eight tokens' loads together
-  for (; e + 7 * 64 < b; e += 8 * 64) {
-    double x[8];
+  // the loads of 8 tokens together
+  auto block = [&](auto with_q) __attribute__((always_inline)) {
+    for (; e + 7 * 64 < b; e += 8 * 64) {
+      float p[8], q[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) x[u] = verify_weight(v, e + u * 64);
+      for (int u = 0; u < 8; ++u) {
+        p[u] = v.p[e + u * 64];
+        q[u] = 0.f;
+        if constexpr (decltype(with_q)::value) q[u] = v.q[e + u * 64];
+      }
 #pragma unroll
-    for (int u = 0; u < 8; ++u) w[u & 3] += x[u];
-  }
+      for (int u = 0; u < 8; ++u) {
+        const double d = (double)p[u] - (double)q[u];
+        w[u & 3] += e + u * 64 != v.skip && d > 0.0 ? d : 0.0;
+      }
+    }
+  };
+  if (v.q) block(std::true_type());
+  else block(std::false_type());
   for (; e < b; e += 64) w[0] += verify_weight(v, e);
   return wave_sum_f64((w[0] + w[1]) + (w[2] + w[3]));
 }
@@ -233,7 +246,7 @@ __global__ void __launch_bounds__(VERIFY_WAVES * 64) verify_kernel(VerifyArgs P)
 }
 
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s) {
-  if (a.vocab <= VERIFY_ONE) {
+  if (verify_one(a.b, a.vocab)) {
     verify_kernel<false><<<a.b, VERIFY_WAVES * 64, 0, s>>>(a);
   } else {
     verify_sum_kernel<<<dim3(VERIFY_WAVES, a.b), 256, 0, s>>>(a);

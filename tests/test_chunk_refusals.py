@@ -142,9 +142,10 @@ def test_verify(L):
     for k in ("target", "tokens", "draft_start", "u_accept", "u_sample", "out", "acc"):
         assert call(**{k: None}) == BAD
     assert call(draft=0x1001) == BAD
-    assert call(V=32769, ws=None) == WS and call(V=32769, n=4095) == WS
-    assert L.sas_workspace_size(None, sas.OP_VERIFY_DRAFTS, 2, 32769) == 4096
-    assert L.sas_workspace_size(None, sas.OP_VERIFY_DRAFTS, 2, 32768) == 0
+    assert call(V=65537, ws=None) == WS and call(V=65537, n=4095) == WS
+    assert L.sas_workspace_size(None, sas.OP_VERIFY_DRAFTS, 2, 65537) == 4096
+    assert L.sas_workspace_size(None, sas.OP_VERIFY_DRAFTS, 2, 65536) == 0
+    assert L.sas_workspace_size(None, sas.OP_VERIFY_DRAFTS, 128, 65537) == 0
     assert L.sas_workspace_size(None, sas.OP_ATTENTION_CHUNK, 3, 4) == 0
 
 

@@ -38,11 +38,11 @@ def check(args, D):
     return want, acc
 
 
-@pytest.mark.parametrize("V", [1, 2, 255, 256, 257, 1000, 8193, 32768, 32769, 100003])
+@pytest.mark.parametrize("V", [1, 2, 255, 256, 257, 1000, 8193, 32768, 65536, 65537, 100003])
 @pytest.mark.parametrize("drafts", [[3], [0], [0, 1, 5, 2, 7], [4] * 40], ids=str)
 @pytest.mark.parametrize("with_q", [True, False])
 def test_against_the_oracle(V, drafts, with_q):
-    if V == 100003 and len(drafts) > 10:
+    if V > 40000 and len(drafts) > 10:
         drafts = drafts[:6]
     print(f"\n[case] verify V={V} drafts={drafts} q={with_q}", flush=True)
     for seed in range(3):
@@ -50,6 +50,11 @@ def test_against_the_oracle(V, drafts, with_q):
         if not with_q:
             a[1] = None
         check(a, max(drafts) + seed)
+
+
+@pytest.mark.parametrize("b", [127, 128])
+def test_many_sequences_of_a_large_vocabulary(b):
+    check(case([i % 3 for i in range(b)], 70001, b), 2)
 
 
 def test_more_drafts_than_a_wave():
