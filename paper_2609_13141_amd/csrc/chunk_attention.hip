@@ -16,8 +16,8 @@
 //
 // The tile loop is that of the prefill kernel (S^T = K Q^T, P^T fed back from
 // registers as the B operand of O^T = V^T P^T) with rows found through the
-// block table: a wave holds the page of key l of the next tile in lane l, one
-// load per tile, and gives it to the copying lanes with a permute.
+// block table: a wave loads the entries of a tile's keys once, a tile ahead, and
+// copies the rows of a page from one scalar address.
 #include <float.h>
 #include <stdint.h>
 
@@ -36,7 +36,7 @@ constexpr float LN2 = 0.6931471805599453f;
 typedef __attribute__((address_space(3))) void chunk_lds_t;
 
 // Keys of a tile: 64 in bf16, 32 in fp32 (the same bytes).  LEAST: tiles of the shortest
-// part.  An fp32 tile takes 2.9 us, more than another part's merge: 4 sequences of up to 60
+// part.  An fp32 tile takes 2.9 us, more than another part's merge: 3 sequences of up to 50
 // new tokens over up to 200 keys take 14.8 us with parts of one tile and 16.3 with two.  A
 // bf16 tile takes less, and parts of one tile gained nothing.
 template <typename T> struct ChunkTile;
@@ -471,6 +471,10 @@ __device__ __forceinline__ uint2 chunk_read_tr(lds_s16x4_t* __restrict p) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(p));
 }
 
+// One job: a tile's rows over one part of its keys, two tiles of keys in LDS by turns, one
+// barrier a tile.  Bound by the keys' bytes where rows are few: one row over 131000 cached
+// (32/32 heads of 128, 2.1 GB) 359 us, 6.0 TB/s; 32 sequences of 5 new tokens over up to
+// 16000 (28/4 heads, 280 MB) 50 us, 5.6 TB/s, of which 4.7 us pass before the first key.
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   constexpr bool BF = sizeof(T) == 2;
@@ -1018,7 +1022,8 @@ __global__ void __launch_bounds__(256, 2) chunk_attn_kernel(ChunkArgs P, int res
 }
 
 // Merge of divided tiles: a wave per (row, head), its lanes 64 / C8 parts at a time x
-// 8 dimensions each.
+// 8 dimensions each.  Bound by its two rounds of loads: 160 rows of 28 heads 6.0 us (7.0
+// with four rounds).
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(ChunkArgs P) {
   constexpr int C8 = DH / 8, PG = 64 / C8;
