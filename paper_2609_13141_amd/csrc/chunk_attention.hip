@@ -320,8 +320,8 @@ __device__ __forceinline__ void chunk_copy(const ChunkArgs& P, const void* pool,
       chunk_copy_piece<0>(rows, d, at(0));
       chunk_copy_piece<1024>(rows, d, at(1));
       if constexpr (NL > 2) {
-        chunk_copy_piece<2048>(rows, d, at(2));
-        chunk_copy_piece<3072>(rows, d, at(3));
+        chunk_copy_piece<2 * 1024>(rows, d, at(2));
+        chunk_copy_piece<3 * 1024>(rows, d, at(3));
       }
     } else {
 #pragma unroll
@@ -779,8 +779,8 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
     chunk_copy_piece<0>(rows, d, at[0]);
     chunk_copy_piece<1024>(rows, d, at[1]);
     if constexpr (NL > 2) {
-      chunk_copy_piece<2048>(rows, d, at[2]);
-      chunk_copy_piece<3072>(rows, d, at[3]);
+      chunk_copy_piece<2 * 1024>(rows, d, at[2]);
+      chunk_copy_piece<3 * 1024>(rows, d, at[3]);
     }
   };
   auto load_k = [&](int kt, uint64_t off) { copy(P.k_pages, tiles + ((kt - tlo) & 1) * TB, off); };
