@@ -523,7 +523,9 @@ typedef struct {
 
 /* Outputs of sas_plan_chunk, all DEVICE and required; none may be an input.
  *  row_start [b+1]  rows of the sequences; tokens past `rows` have no row
- *  kv_len [b]       ctx_len + new_len
+ *  kv_len [b]       ctx_len + the sequence's rows: less than ctx_len + new_len where
+ *                   tokens have no row (they are not in the chunk, and their pages are
+ *                   there for the next one)
  *  seq, pos [rows]  the row's sequence and position, -1 in padding rows
  *  slot [rows] int64  page * page_size + offset of the row's key and value in the
  *                   pool, -1 where the position has no page, and in padding rows

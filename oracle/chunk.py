@@ -42,8 +42,9 @@ def plan_chunk(ctx_len, new_len, held, free_pages, free_count, table, page_size,
                 table[i, j] = -1
                 missing += 1
         have.append(got)
-        kv.append(min(c + m, 2 ** 31 - 1))
-        for j in range(min(m, max(rows - total, 0))):
+        given = min(m, max(rows - total, 0))   # tokens past `rows` have no row, and are not in the chunk
+        kv.append(min(c + given, 2 ** 31 - 1))
+        for j in range(given):
             r, p = total + j, c + j
             page = int(table[i, p // page_size]) if p // page_size < width else -1
             seq[r], pos[r] = i, min(p, 2 ** 31 - 1)

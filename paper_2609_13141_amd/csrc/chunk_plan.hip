@@ -101,7 +101,8 @@ __global__ void __launch_bounds__(PLAN_NT) plan_chunk_kernel(PlanArgs P) {
       break;
     }
     const PlanSeq q = plan_seq(P, i);
-    P.kv_len[i] = (int)min((long long)q.ctx + q.m, 0x7fffffffll);
+    // (tokens without a row are not in the chunk: attention places a sequence's rows from its end)
+    P.kv_len[i] = (int)min((long long)q.ctx + (row0[i + 1] - row0[i]), 0x7fffffffll);
     P.held_out[i] = q.held + (int)min((long long)q.need, max(avail - page0[i], 0ll));
   }
   // table entries of the pages wanted, off the top of the stack in the sequences' order

@@ -669,10 +669,11 @@ def _rotary(cfg: Config, pos, gain_q, gain_k, sections, rows: int, dev) -> Rotar
 
 def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free_count, rows: int) -> dict:
     """Pages and slots of a chunk: ctx_len, new_len, pages_held [b], the stack
-    free_pages [capacity] with free_count [1] entries (all int32); `rows` rows
-    (at least the sum of new_len, or tokens go without).  Writes the new entries
-    of cache.block_table and returns row_start [b+1], kv_len [b], seq and pos
-    [rows], slot [rows] (int64), pages_held [b], free_count [1], missing [1]."""
+    free_pages [capacity] with free_count [1] entries (all int32); `rows` rows.
+    Where new_len sum to more, the last tokens have no row and are left to a later
+    chunk: kv_len is ctx_len plus the sequence's rows.  Writes the new entries of
+    cache.block_table and returns row_start [b+1], kv_len [b], seq and pos [rows],
+    slot [rows] (int64), pages_held [b], free_count [1], missing [1]."""
     dev = _device("ctx_len", ctx_len)
     _count("rows", rows, 1)
     b = ctx_len.numel()
