@@ -816,10 +816,12 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
       if (kt * KEYS + j + lk4 > t || !((vm >> j) & 1)) s[v] = -INFINITY;
     }
   };
-  // The reference of the exponentials.  Any gives the same sums, so it is looked at only
-  // where a lane's 16 weights add up to more than `limit`: one of them then exceeds 2^8
-  // (or is the first of its row), and the reference moves to the row's maximum.
-  float limit = 0.f;
+  // The reference of the exponentials.  Any that they do not all underflow against gives the
+  // same sums, so it is looked at only where a lane's 16 weights add up to more than `limit`:
+  // one of them then exceeds 2^8, and the reference moves to the row's maximum.  A row that
+  // has none yet is looked at whatever the sum (0 may be underflow), one that attends nothing
+  // never for being empty.
+  float limit = t < 0 ? 4096.f : -1.f;
   auto reference = [&](const floatx16_t& s) __attribute__((always_inline)) {
     float mx = s[0];
 #pragma unroll
