@@ -37,7 +37,7 @@ class Stack:
                        for l in range(len(layers))]
         self.ws = sas.Workspace(device)
         self.max_len = max_len
-        self.pos = None
+        self.pos = None     # cached tokens of every sequence: a number, after extend a device tensor [b]
 
     def prefill(self, ids, img=None, *, logits: bool = False, on_layer=None):
         """ids [b, n] int32 on the device (-1 = next image embedding row);
@@ -57,8 +57,12 @@ class Stack:
         return (tok, lg) if logits else tok
 
     def positions(self, steps: int):
-        """Device position vectors for the next `steps` decode steps."""
+        """Device position vectors for the next `steps` decode steps, behind the prompt,
+        the last `extend` and the steps since.  (A replayed graph moves nothing here, and
+        after drafts that were not accepted the lengths are the caller's to know.)"""
         b = self.w.batch
+        if isinstance(self.pos, torch.Tensor):
+            return [self.pos + s for s in range(steps)]
         return [torch.full((b,), self.pos + s, dtype=torch.int32, device=self.device) for s in range(steps)]
 
     def step(self, tok, pos, *, logits: bool = False, sel_idx: bool = False, taps: bool = False):
@@ -78,7 +82,7 @@ class Stack:
             sels.append(sel)
         nxt, lg = sas.lm_head_argmax(self.cfg_decode, x, self.ends["rms_final"], self.ends["w_lm"], logits=logits,
                                      ws=self.ws)
-        self.pos += 1
+        self.pos = self.pos + 1
         out = (nxt, lg, (sels if sel_idx else None))
         return out + (tps,) if taps else out
 
@@ -87,7 +91,8 @@ class Stack:
         [rows] int32, sequence i's new_len[i] after each other at positions
         ctx_len[i] .. (ctx_len, new_len [b] int32, all on the device; rows past
         their sum are padding).  Returns the last layer's output [rows, d] and
-        the rows' plan (see sas.plan_chunk)."""
+        the rows' plan (see sas.plan_chunk): kv_len, its lengths after the call, are
+        where the next tokens go."""
         x = sas.embed(self.cfg_prefill, ids.view(1, -1), self.ends["embed"])[0]
         none = torch.zeros(1, dtype=torch.int32, device=ids.device)
         plan = None
@@ -96,6 +101,7 @@ class Stack:
         for W, cache in zip(self.layers, self.caches):
             plan = sas.plan_chunk(cache, ctx_len, new_len, held, none, none, ids.numel())
             x = sas.layer_chunk(self.cfg_prefill, x, W, cache, ctx_len, plan, ws=self.ws)
+        self.pos = plan["kv_len"].clone()
         return x, plan
 
     def logits(self, x):
