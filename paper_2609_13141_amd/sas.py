@@ -236,17 +236,25 @@ def workspace_size(cfg: Config, op: int, batch: int, seq_len: int) -> int:
 
 
 class Workspace:
-    """Grow-only device scratch buffer reused across calls."""
+    """Grow-only device scratch buffer reused across calls.  A buffer that a captured
+    graph writes to when it is replayed stays allocated when a larger one replaces it."""
 
     def __init__(self, device="cuda"):
         self.device = device
         self.buf = None
+        self.captured = False  # self.buf was given out under capture
+        self.kept = []
 
     def get(self, nbytes: int):
         if nbytes == 0:
             return None, 0
         if self.buf is None or self.buf.numel() < nbytes:
+            if self.captured:
+                self.kept.append(self.buf)
             self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.captured = False
+        if not self.captured and self.buf.is_cuda and torch.cuda.is_current_stream_capturing():
+            self.captured = True
         return self.buf, self.buf.numel()
 
 
