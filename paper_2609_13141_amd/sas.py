@@ -639,7 +639,12 @@ def _scratch(ws: Workspace | None, nbytes: int, dev):
     """Scratch to keep until the call has returned: from `ws`, or torch's allocator."""
     if nbytes == 0:  # a configuration that the call will refuse
         nbytes = 16
-    return torch.empty(nbytes, dtype=torch.uint8, device=dev) if ws is None else ws.get(nbytes)[0]
+    if ws is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    buf = ws.get(nbytes)[0]
+    if buf.device != dev:
+        raise SasError(SAS_ERR_INVALID_ARGUMENT, f"ws: scratch on {buf.device}, the tensors are on {dev}")
+    return buf
 
 
 def _cache_arg(cfg: Config, cache: PagedCache, b: int, dev) -> PagedKV:
