@@ -607,7 +607,7 @@ def _need(name: str, t, dtype, shape: tuple, dev) -> int:
 
 
 def _count(name: str, n: int, least: int = 0) -> int:
-    """n, where it fits the C argument."""
+    """n, where it fits the C argument (which would take it modulo 2^32)."""
     if not least <= n < 2 ** 31:
         raise SasError(SAS_ERR_INVALID_ARGUMENT, f"{name} {n} (from {least} to 2^31 - 1)")
     return n
@@ -653,7 +653,8 @@ def _cache_arg(cfg: Config, cache: PagedCache, b: int, dev) -> PagedKV:
     pages = (k.shape[0], Hkv, ps, dh)
     return PagedKV(_need("cache.k_pages", k, act, pages, dev), _need("cache.v_pages", v, act, pages, dev),
                    _need("cache.block_table", t, torch.int32, (b, t.shape[-1]), dev),
-                   _need("cache.k_summary", s, act, (b, Hkv, s.shape[-2], dh), dev), pages[0], ps, t.shape[1], s.shape[2])
+                   _need("cache.k_summary", s, act, (b, Hkv, s.shape[-2], dh), dev), _count("pages", pages[0]), ps,
+                   _count("pages of a sequence", t.shape[1]), _count("blocks of a sequence", s.shape[2]))
 
 
 def _heads_arg(cfg: Config, name: str, t, heads: int, rows: int, dev):
@@ -689,11 +690,11 @@ def plan_chunk(cache: PagedCache, ctx_len, new_len, pages_held, free_pages, free
     slot [rows] (int64), pages_held [b], free_count [1], missing [1]."""
     dev = _device("ctx_len", ctx_len)
     _count("rows", rows, 1)
-    b = ctx_len.numel()
+    b = _count("sequences", ctx_len.numel())
     i32 = torch.int32
     table = cache.block_table
-    kv = PagedKV(None, None, _need("cache.block_table", table, i32, (b, table.shape[-1]), dev), None, cache.k_pages.shape[0],
-                 cache.page_size, table.shape[1], 0)
+    kv = PagedKV(None, None, _need("cache.block_table", table, i32, (b, table.shape[-1]), dev), None,
+                 _count("pages", cache.k_pages.shape[0]), cache.page_size, _count("pages of a sequence", table.shape[1]), 0)
     pi = PlanIn(_need("ctx_len", ctx_len, i32, (b,), dev), _need("new_len", new_len, i32, (b,), dev),
                 _need("pages_held", pages_held, i32, (b,), dev), _need("free_pages", free_pages, i32, (free_pages.numel(),), dev),
                 _need("free_count", free_count, i32, (1,), dev), _count("entries of free_pages", free_pages.numel()))
@@ -755,7 +756,7 @@ def cache_append(cfg: Config, cache: PagedCache, q, k, v, pos, slot, ctx_len, kv
     keys, values and the summaries of the blocks that the chunk completes; returns
     the normed and rotated queries."""
     dev = _device("q", q)
-    rows, b, H, Hkv, dh = q.shape[0], ctx_len.numel(), cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
+    rows, b, H, Hkv, dh = q.shape[0], _count("sequences", ctx_len.numel()), cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
     (qp, qs), (kp, ks) = _heads_arg(cfg, "q", q, H, rows, dev), _heads_arg(cfg, "k", k, Hkv, rows, dev)
     vp, vs = _heads_arg(cfg, "v", v, Hkv, rows, dev)
     rot = _rotary(cfg, pos, gain_q, gain_k, sections, rows, dev)
@@ -777,7 +778,7 @@ def attention_chunk(cfg: Config, q, cache: PagedCache, row_start, kv_len, *, lse
     cache already.  o [rows, H, dh] (`out` when given; rows behind row_start[b] are
     not written) and lse [rows, H] fp32."""
     dev = _device("q", q)
-    rows, b, H = q.shape[0], kv_len.numel(), cfg.n_heads
+    rows, b, H = q.shape[0], _count("sequences", kv_len.numel()), cfg.n_heads
     qp = _need("q", q, _act(cfg), (rows, H, cfg.head_dim), dev)
     rp = _need("row_start", row_start, torch.int32, (b + 1,), dev)
     kl = _need("kv_len", kv_len, torch.int32, (b,), dev)
@@ -799,7 +800,7 @@ def layer_chunk(cfg: Config, x, W: dict, cache: PagedCache, ctx_len, plan: dict,
     this cache) of ctx_len [b]; pos [axes, rows] int32 are the rotary positions (None:
     the plan's).  Appends the chunk to the cache; returns y [rows, d]."""
     dev = _device("x", x)
-    rows, b = x.shape[0], ctx_len.numel()
+    rows, b = x.shape[0], _count("sequences", ctx_len.numel())
     i32 = torch.int32
     xp = _need("x", x, _act(cfg), (rows, cfg.d_model), dev)
     y = torch.empty_like(x)
@@ -823,10 +824,10 @@ def verify_drafts(target, draft, tokens, draft_start, u_accept, u_sample, max_dr
     fp32 uniforms.  tokens [b, max_draft + 1]: the accepted ones, the drawn one,
     -1; accepted [b]."""
     dev = _device("target", target)
-    rows, b = tokens.numel(), u_sample.numel()
+    rows, b = tokens.numel(), _count("sequences", u_sample.numel())
     f32, i32 = torch.float32, torch.int32
     _count("max_draft", max_draft), _count("rows", rows)
-    V = target.shape[-1]
+    V = _count("vocab", target.shape[-1])
     tp = _need("target", target, f32, (rows + b, V), dev)
     dp = None if draft is None else _need("draft", draft, f32, (rows, V), dev)
     vi = VerifyIn(tp, dp or None, _need("tokens", tokens, i32, (rows,), dev),
