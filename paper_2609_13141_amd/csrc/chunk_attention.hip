@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_
 #pragma unroll
     for (int u = 0; u < MAX_PER; ++u) v += f(w[u]);
     long long total;
-    (void)scan1024((long long)v, s, total);  // (whole numbers)
+    (void)scan1024((long long)fmin(v, 0x1p52), s, total);  // (whole numbers; offsets that break the rules may give more)
     return (double)total;
   });
   long long jobs = 0, prows = 0;
@@ -208,6 +208,9 @@ __global__ void __launch_bounds__(1024) chunk_plan_kernel(ChunkArgs P, int keys_
     j0 += w[u].units * parts;
     if (parts > 1) r0 += w[u].units * parts * w[u].prow;
   }
+  // sequences that do not overlap have at most 2^24 jobs or so: overlapping ones past 31
+  // bits of them are not done
+  if (njobs > INT32_MAX) njobs = nrows = 0;
   if (tid == 0) {
     P.head[0] = (int)njobs;
     P.head[1] = nrows > 0;
