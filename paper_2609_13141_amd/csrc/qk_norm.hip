@@ -40,13 +40,14 @@ __device__ __forceinline__ QkPair qk_pair(const QkArgs& P, int lane) {
   r.axis = P.axes == 1 || i < P.sec0 ? 0 : i < P.sec0 + P.sec1 ? 1 : 2;
   return r;
 }
-// cos and sin of the pair's angle: the fraction of a turn is taken in fp64
+// cos and sin of the pair's angle: the fraction of a turn is taken in fp64, and what its
+// rounding to fp32 leaves off (2^-26 of a turn, 10^-7 rad) turns the result by first order
 __device__ __forceinline__ float2 qk_turn(const QkPair& pr, int pos) {
-  const double a = (double)pos * pr.freq;
-  const float f = (float)(a - rint(a));
+  const double a = (double)pos * pr.freq, t = a - rint(a);
+  const float f = (float)t, rest = (float)(t - (double)f) * 6.28318530717958647693f;
   float s, c;
   sincospif(2.f * f, &s, &c);
-  return make_float2(c, s);
+  return make_float2(fmaf(-rest, s, c), fmaf(rest, c, s));
 }
 
 template <typename T>
