@@ -669,7 +669,7 @@ typedef struct {
  * or NaN count as zero.
  * out_tokens [b, max_draft + 1] int32: the accepted tokens, the drawn one, -1;
  * accepted [b] int32.  ws: sas_workspace_size(NULL, SAS_OP_VERIFY_DRAFTS, batch,
- * vocab), 0 for vocabularies up to 65536 and from 128 sequences on. */
+ * vocab), 0 for vocabularies up to 65536, and up to 131072 from 128 sequences on. */
 sas_status sas_verify_drafts(int32_t batch, int32_t rows, int32_t vocab, int32_t max_draft, const sas_verify_in* in,
                              int32_t* out_tokens, int32_t* accepted, void* ws, size_t ws_bytes, void* stream);
 

@@ -459,8 +459,18 @@ struct VerifyArgs {
   int32_t *out, *accepted;         // [b, max_draft + 1], [b]
   double* part;                    // [b, 16, 16] sums of pieces, where verify_one does not hold
 };
-// Whether a workgroup a sequence does it all.
-inline bool verify_one(int b, int vocab) { return vocab <= 65536 || b >= 128; }
+// Whether a workgroup a sequence does it all, rather than sixteen that take the sums of
+// the first two cuts before it.  The second launch pays for large vocabularies: of fewer
+// sequences than half the compute units (the rest would idle), and of any number where a
+// row takes longer to read than a launch.  Captured, rows not in the L2s, one workgroup
+// and two kernels, us:
+//     tokens      8 sequences    64            112           128           256 or 320
+//     50000       13.7  13.4     17.1  16.6                  17.7  20.8    21.3  29.6
+//     65537       15.8  13.8     18.8  16.8    21.0  20.1    18.5  20.5    36.3  37.4
+//     100003      23.7  14.4     25.1  17.8    24.0  21.9    25.3  23.3    34.9  35.2
+//     131072                                   29.1  24.5    25.0  26.0    63.4  59.1
+//     250000      46.9  19.8     48.2  28.3                  62.4  46.2    91.4  88.4
+constexpr bool verify_one(int b, int vocab) { return vocab <= 65536 || (b >= 128 && vocab <= 131072); }
 inline size_t verify_scratch_bytes(int b, int vocab) { return verify_one(b, vocab) ? 0 : (size_t)b * 256 * sizeof(double); }
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t s);
 

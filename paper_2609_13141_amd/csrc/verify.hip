@@ -10,10 +10,7 @@
 // vocabulary is cut in sixteen, the sixteenth that the uniform falls into in sixteen
 // again, until a wave can scan it token by token (eight a lane, loaded together; 64 at a
 // time 2.4 us more of 29, all waves scanning another 1).  A workgroup a sequence does it
-// all; where few sequences have large vocabularies, sixteen take a sequence's sums first
-// (captured, one workgroup and two kernels):
-//   8 x 32000: 10.2 and 11.7 us, 8 x 65536: 12.7 and 13.0, 8 x 100003: 16.7 and 15.1;
-//   128 x 50000: 17.1 and 20.6, 128 x 100003 (102 MB): 25.3 and 26.4.
+// all; for large vocabularies sixteen take a sequence's sums first (verify_one).
 // Differences and sums are fp64: the fp32 inputs' products and differences are exact
 // there, and a token's border in the CDF is some 1e-16 wide rather than the 1e-7 of an
 // fp32 sum.
@@ -25,7 +22,7 @@
 namespace sas {
 
 constexpr int VERIFY_WAVES = 16;  // and pieces of a cut
-constexpr int VERIFY_LANE = 8;    // tokens of a lane in the last one
+constexpr int VERIFY_LANE = 8;    // tokens that a lane loads together
 
 // tokens of a piece of n, whole steps of a wave
 __host__ __device__ __forceinline__ int verify_piece(int n) { return ((n + VERIFY_WAVES - 1) / VERIFY_WAVES + 63) / 64 * 64; }
@@ -71,42 +68,41 @@ __device__ __forceinline__ VerifyRow verify_row(const VerifyArgs& P, int i) {
   return v;
 }
 
-// weight of token e (negative and NaN ones count as zero)
-__device__ __forceinline__ double verify_weight(const VerifyRow& v, int e) {
-  const double w = (double)v.p[e] - (v.q ? (double)v.q[e] : 0.0);
-  return e != v.skip && w > 0.0 ? w : 0.0;
-}
-
 __device__ __forceinline__ double wave_sum_f64(double x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
   return x;
 }
 
-// sum of the weights of tokens [a, b), a lane every 64th
+// sum of the weights of tokens [a, b) (negative and NaN ones count as zero), a lane every 64th
 __device__ __forceinline__ double verify_sum(const VerifyRow& v, int a, int b) {
   double w[4] = {0.0, 0.0, 0.0, 0.0};
   int e = a + (threadIdx.x & 63);
-  // the loads of 8 tokens together
-  auto block = [&](auto with_q) __attribute__((always_inline)) {
-    for (; e + 7 * 64 < b; e += 8 * 64) {
-      float p[8], q[8];
+  // the loads of 8 tokens together, also of fewer (those past the end load the last token,
+  // without weight): one at a time, pieces of less than 512 tokens made the kernel before
+  // slower than the one workgroup (8 x 100003: 21.5 -> 14.4 us)
+  auto block = [&](auto with_q, int last) __attribute__((always_inline)) {
+    float p[8], q[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        p[u] = v.p[e + u * 64];
-        q[u] = 0.f;
-        if constexpr (decltype(with_q)::value) q[u] = v.q[e + u * 64];
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const double d = (double)p[u] - (double)q[u];
-        w[u & 3] += e + u * 64 != v.skip && d > 0.0 ? d : 0.0;
-      }
+    for (int u = 0; u < 8; ++u) {
+      const int x = min(e + u * 64, last);
+      p[u] = v.p[x];
+      q[u] = 0.f;
+      if constexpr (decltype(with_q)::value) q[u] = v.q[x];
     }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const double d = (double)p[u] - (double)q[u];
+      w[u & 3] += e + u * 64 <= last && e + u * 64 != v.skip && d > 0.0 ? d : 0.0;
+    }
+    e += 8 * 64;
   };
-  if (v.q) block(std::true_type());
-  else block(std::false_type());
-  for (; e < b; e += 64) w[0] += verify_weight(v, e);
+  auto all = [&](auto with_q) __attribute__((always_inline)) {
+    while (e + 7 * 64 < b) block(with_q, 0x7fffffff);
+    if (e < b) block(with_q, b - 1);
+  };
+  if (v.q) all(std::true_type());
+  else all(std::false_type());
   return wave_sum_f64((w[0] + w[1]) + (w[2] + w[3]));
 }
 

@@ -111,3 +111,10 @@ def test_captured_replays(V):
         want, acc = oracle.chunk.verify_drafts(*[t.numpy() for t in b], 2)
         np.testing.assert_array_equal(out["tokens"].cpu().numpy(), want)
         np.testing.assert_array_equal(out["accepted"].cpu().numpy(), acc)
+
+
+@pytest.mark.parametrize("V,b,scratch", [(65536, 3, False), (65537, 127, True), (65537, 128, False), (131072, 129, False),
+                                         (131073, 128, True), (131073, 1, True), (250001, 130, True)])
+def test_both_sides_of_the_division(V, b, scratch):
+    check(case([i % 2 for i in range(b)], V, b), 2)
+    assert (sas.lib().sas_workspace_size(None, sas.OP_VERIFY_DRAFTS, b, V) > 0) == scratch
