@@ -11,9 +11,10 @@
 // again, until a wave can scan it token by token (eight a lane, loaded together; 64 at a
 // time 2.4 us more of 29, all waves scanning another 1).  A workgroup a sequence does it
 // all; for large vocabularies sixteen take a sequence's sums first (verify_one).
-// Differences and sums are fp64: the fp32 inputs' products and differences are exact
-// there, and a token's border in the CDF is some 1e-16 wide rather than the 1e-7 of an
-// fp32 sum.
+// Products, differences and sums are fp64: products of the fp32 inputs are exact there,
+// differences and sums are rounded, so that a token's border in the CDF is uncertain by a
+// few 1e-16 of the sum (an fp32 sum's by 1e-7).  The forms add in different orders: a
+// uniform that close to a border may draw either neighbour, by the number of sequences.
 #include <type_traits>
 
 #include "common.h"
