@@ -653,11 +653,12 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
       }
       __builtin_amdgcn_s_setprio(2);
       if constexpr (BF) {
-        // P goes to the matrix unit as two bf16 numbers, the rounded weight and the rest of it
-        // (together within 2^-16 of the weight), so that a token here is as exact as in the
-        // decode step.  The calls of this loop are bound by the keys' bytes, and the second
-        // product nearly hides behind them: 366 -> 369 us for one row over 131000 cached, 64.6
-        // -> 65.6 for 32 sequences of 5.
+        // P goes to the matrix unit as two bf16 numbers, the weight's upper half and the rest of
+        // it (together within 2^-16 of the weight), so that a token here is as exact as in the
+        // decode step.  The rest is kept positive (2^-20 of the weight at least): 0, or less
+        // behind a half rounded up, would turn an infinite value into NaN.  The calls of this
+        // loop are bound by the keys' bytes, and the second product nearly hides behind them:
+        // 366 -> 371 us for one row over 131000 cached, 64.5 -> 66.0 for 32 sequences of 5.
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
           const int st = ks >> 1, v0 = 8 * (ks & 1);
@@ -665,8 +666,9 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float a = s[st][v0 + 2 * j], b = s[st][v0 + 2 * j + 1];
-            hi4[j] = pack_bf16x2(a, b);
-            lo4[j] = pack_bf16x2(a - __uint_as_float(hi4[j] << 16), b - __uint_as_float(hi4[j] & 0xffff0000u));
+            const uint32_t a1 = __float_as_uint(a) & 0xffff0000u, b1 = __float_as_uint(b) & 0xffff0000u;
+            hi4[j] = a1 >> 16 | b1;
+            lo4[j] = pack_bf16x2(fmaxf(a - __uint_as_float(a1), a * 0x1p-20f), fmaxf(b - __uint_as_float(b1), b * 0x1p-20f));
           }
           const uint4 pu = make_uint4(hi4[0], hi4[1], hi4[2], hi4[3]), pr = make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]);
           uint4 vu[DH / 32];

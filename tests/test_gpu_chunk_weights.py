@@ -1,8 +1,8 @@
 """Chunk attention of few rows keeps its weights: outputs that cancel to nearly nothing
 are as exact as the fp32 sums allow, like those of the decode step.
 
-The weights reach the second product within 2^-16 (a bf16 number and the bf16 rest of
-it, half a step of 2^-7 each); logits are off by (dh + 4) 2^-24 sum |q||k| sm, the
+The weights reach the second product within 2^-16 (the upper half, a bf16 number, and
+the rest, less than 2^-7, rounded to bf16); logits are off by (dh + 4) 2^-24 sum |q||k| sm, the
 exponential by as much again, sums of n weighted values by 2^-24 (n / 8 + 64); then one
 rounding of the result, 2^-8 of it."""
 import numpy as np
@@ -31,3 +31,43 @@ def test_single_tokens_and_drafts(ctx, new, H, Hkv, dh, ps):
     bound = A * w + 2.0 ** -8 * np.abs(o) * (1 + w) + 1e-30
     bad = ~(np.abs(got - o) <= bound)
     assert not bad.any(), (int(bad.sum()), bad.size, float((np.abs(got - o) / bound).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 5, 200])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_infinite_values_of_keys_that_every_row_attends(new, bad, dtype):
+    # in tiles far before the diagonal, at weights that are and are not bf16 numbers
+    cfg = config(4, 2, 128, 64, dtype)
+    c = Chunk([500], [new], 4, 2, 128, 16, 64, dtype, seed=111)
+    clean = sas.attention_chunk(cfg, c.q, c.cache, c.row_start, c.kv_len)["o"]
+    for p, d in ((3, 7), (70, 8), (200, 9)):
+        c.cache.v_pages[int(c.cache.block_table[0, p // 16]), :, p % 16, d] = bad
+    c.cache.k_pages[int(c.cache.block_table[0, 70 // 16]), :, 70 % 16] = 0.0    # (a logit of 0)
+    for q in (c.q, torch.zeros_like(c.q)):      # zero queries: weights of one each
+        o = sas.attention_chunk(cfg, q, c.cache, c.row_start, c.kv_len)["o"].float()
+        got = o[..., 7:10]
+        assert torch.isnan(got).all() if bad != bad else (got == bad).all()
+        keep = [e for e in range(128) if not 7 <= e < 10]
+        assert torch.isfinite(o[..., keep]).all()
+    assert torch.isfinite(clean).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 5, 200])
+def test_the_largest_values_in_masked_places(new, dtype):
+    # behind the causal mask, behind the last key and in pages that are not mapped
+    cfg = config(4, 2, 128, 64, dtype)
+    c = Chunk([300], [new], 4, 2, 128, 16, 64, dtype, seed=112, unmap=[(0, 2)], spare_pages=4)
+    c.cache.k_pages.nan_to_num_(0.0), c.cache.v_pages.nan_to_num_(0.0)
+    clean = sas.attention_chunk(cfg, c.q, c.cache, c.row_start, c.kv_len)["o"]
+    top = torch.finfo(c.q.dtype).max
+    far = torch.ones(c.cache.v_pages.shape[0], 16, dtype=torch.bool, device="cuda")
+    p = torch.arange(300 + min(new, 3), device="cuda")
+    pg = c.cache.block_table[0, p // 16].long()
+    far[pg[pg >= 0], (p % 16)[pg >= 0]] = False      # (rows up to the third attend these)
+    for pool in (c.cache.k_pages, c.cache.v_pages):
+        pool.copy_(torch.where(far[:, None, :, None], top, pool))
+        pool[..., 1::2].copy_(torch.where(far[:, None, :, None], -top, pool[..., 1::2]))
+    o = sas.attention_chunk(cfg, c.q, c.cache, c.row_start, c.kv_len)["o"]
+    assert torch.equal(o[:3], clean[:3])
