@@ -603,7 +603,8 @@ sas_status sas_qk_norm_rope_backward(const sas_config* cfg, int32_t rows, const 
  * head's key and value may be either's); then the summaries of the blocks that positions
  * ctx_len[i] .. kv_len[i] - 1 complete are written to cache->k_summary (mean of
  * the block's keys in the pages, projected by w_gk [Hkv, dh, dh] when given).
- * q_out may be in->q itself when that is contiguous. */
+ * q_out may be in->q itself when that is contiguous.  (Which later calls can go on
+ * with keys that have gains or several axes: see sas_layer_chunk.) */
 sas_status sas_cache_append(const sas_config* cfg, int32_t batch, int32_t rows, const sas_rotary* rot,
                             const sas_qkv* in, const int64_t* slot, const int32_t* ctx_len, const int32_t* kv_len,
                             const void* w_gk, const sas_paged_kv* cache, void* q_out, void* stream);
@@ -613,7 +614,10 @@ sas_status sas_cache_append(const sas_config* cfg, int32_t batch, int32_t rows, 
  * t = kv_len[i] - m + j and attends every mapped position up to t (the dense
  * prefill of Sec. 5.1 over a cache; cfg->mode is not read).
  * q, o [rows, H, dh], apart; lse [rows, H] fp32 or NULL.  A row that attends nothing
- * gives o = 0, lse = -inf.  H / Hkv <= 128; the block table covers at most 2^30
+ * gives o = 0, lse = -inf.  bf16: where the average sequence fills a tile of 128 rows
+ * (tokens x heads of a kv head; pages of 16 or more), the weights are rounded to bf16
+ * for the product with the values, as in the whole-prompt attention; otherwise they
+ * keep 16 bits and more (within 2^-16), as in the decode step.  H / Hkv <= 128; the block table covers at most 2^30
  * positions.  ws: sas_workspace_size(cfg, SAS_OP_ATTENTION_CHUNK, batch, rows),
  * of which all but the last 65 MiB (fewer for dh = 64), where parts of divided
  * work are joined, is needed. */
@@ -635,7 +639,9 @@ typedef struct {
  * rotated by rot and appended to the cache (sas_cache_append, w->w_gk projecting the
  * summaries); attention over the cache (sas_attention_chunk); h1 = x + O W_o^T;
  * y = h1 + SwiGLU(RMSNorm(h1)).  w->w_gq and w->decode_packed are not read.  Padding
- * rows give unspecified outputs.  ws: sas_workspace_size(cfg, SAS_OP_LAYER_CHUNK,
+ * rows give unspecified outputs.  sas_layer_forward and sas_decode_step know one axis
+ * and no head norm: a cache that holds keys with gains, or turned by more than the
+ * sequence's positions, is gone on with by this call (single tokens as chunks of one).  ws: sas_workspace_size(cfg, SAS_OP_LAYER_CHUNK,
  * batch, rows); its last part, for partial sums, may be shorter or left out. */
 sas_status sas_layer_chunk(const sas_config* cfg, int32_t batch, int32_t rows, const void* x,
                            const sas_layer_weights* w, const sas_rotary* rot, const sas_chunk* chunk,

@@ -906,7 +906,10 @@ __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int se
           const uint2 hi = chunk_read_tr((lds_s16x4_t*)(uintptr_t)((o_tr[1] ^ (dt << 6)) + vb + (2 * st + ks) * 16 * RB));
           f[dt] = make_uint4(lo.x, lo.y, hi.x, hi.y);
         };
-        // P is rounded to bf16 for the matrix instruction; the sum keeps the fp32 weights
+        // P is rounded to bf16 for the matrix instruction (2^-8 of a weight, averaged over the
+        // keys; the whole-prompt attention does the same), the sum keeps the fp32 weights: a
+        // second product with the rest, as in the plain loop, takes 2048 over 30005 from 0.907
+        // to 1.254 ms
         auto finish = [&](int u) {
 #pragma unroll
           for (int v = u * PER; v < (u + 1) * PER; v += 2) {

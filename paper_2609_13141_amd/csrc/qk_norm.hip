@@ -157,8 +157,9 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs P, int parts, 
 // As many workgroups as stay resident walk the units (a row's group of heads) in
 // runs of QK_RUN, so that a wave forms a row's angles once for several; it loads its
 // next unit before it computes the current one.  Lanes keep the
-// gains' gradients of their 16 dimensions in fp32 registers and leave one sum per
-// workgroup, added in a fixed order by qk_gain_sum_kernel.
+// gains' gradients of their 16 dimensions in fp32 registers (a term for each of a lane's
+// units: 43 at 16384 rows of 32/32 heads, where the result is 1.6e-7 off in norm) and
+// leave one fp32 sum per workgroup, added in fp64 and a fixed order by qk_gain_sum_kernel.
 // Measured at 16384 rows of 32/32 heads of 128 (bf16; 805 MB): 196 us with 1024
 // workgroups of two units at a time and no loads ahead, 168 us with the 768 that are
 // resident, 162 us with the next unit's loads ahead, 160 us (5.0 TB/s; a copy reaches

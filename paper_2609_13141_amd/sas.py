@@ -798,7 +798,9 @@ def layer_chunk(cfg: Config, x, W: dict, cache: PagedCache, ctx_len, plan: dict,
                 sections=None, ws: Workspace | None = None):
     """One decoder layer over a chunk's rows x [rows, d]: plan is plan_chunk's (for
     this cache) of ctx_len [b]; pos [axes, rows] int32 are the rotary positions (None:
-    the plan's).  Appends the chunk to the cache; returns y [rows, d]."""
+    the plan's).  Appends the chunk to the cache; returns y [rows, d].  layer_forward and
+    decode_step know neither gains nor other positions: a cache filled with them is gone
+    on with by layer_chunk."""
     dev = _device("x", x)
     rows, b = x.shape[0], _count("sequences", ctx_len.numel())
     i32 = torch.int32
