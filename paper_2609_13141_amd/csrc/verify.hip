@@ -79,28 +79,32 @@ __device__ __forceinline__ double wave_sum_f64(double x) {
 __device__ __forceinline__ double verify_sum(const VerifyRow& v, int a, int b) {
   double w[4] = {0.0, 0.0, 0.0, 0.0};
   int e = a + (threadIdx.x & 63);
-  // the loads of 8 tokens together, also of fewer (those past the end load the last token,
-  // without weight): one at a time, pieces of less than 512 tokens made the kernel before
-  // slower than the one workgroup (8 x 100003: 21.5 -> 14.4 us)
-  auto block = [&](auto with_q, int last) __attribute__((always_inline)) {
-    float p[8], q[8];
+  // the loads of 8 tokens together, also of the last ones (those past the end load the last
+  // token, without weight; a batch of 2 where that is enough): one at a time, pieces of less
+  // than 512 tokens made the kernel before slower than the one workgroup (8 x 100003: 21.5
+  // -> 14.4 us)
+  auto batch = [&](auto with_q, auto width, int last) __attribute__((always_inline)) {
+    constexpr int N = decltype(width)::value;
+    float p[N], q[N];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < N; ++u) {
       const int x = min(e + u * 64, last);
       p[u] = v.p[x];
       q[u] = 0.f;
       if constexpr (decltype(with_q)::value) q[u] = v.q[x];
     }
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < N; ++u) {
       const double d = (double)p[u] - (double)q[u];
       w[u & 3] += e + u * 64 <= last && e + u * 64 != v.skip && d > 0.0 ? d : 0.0;
     }
-    e += 8 * 64;
+    e += N * 64;
   };
   auto all = [&](auto with_q) __attribute__((always_inline)) {
-    while (e + 7 * 64 < b) block(with_q, 0x7fffffff);
-    if (e < b) block(with_q, b - 1);
+    const std::integral_constant<int, 8> eight;
+    while (e + 7 * 64 < b) batch(with_q, eight, 0x7fffffff);
+    if (e + 2 * 64 < b) batch(with_q, eight, b - 1);
+    else if (e < b) batch(with_q, std::integral_constant<int, 2>(), b - 1);
   };
   if (v.q) all(std::true_type());
   else all(std::false_type());
