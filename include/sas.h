@@ -614,10 +614,10 @@ sas_status sas_cache_append(const sas_config* cfg, int32_t batch, int32_t rows, 
  * t = kv_len[i] - m + j and attends every mapped position up to t (the dense
  * prefill of Sec. 5.1 over a cache; cfg->mode is not read).
  * q, o [rows, H, dh], apart; lse [rows, H] fp32 or NULL.  A row that attends nothing
- * gives o = 0, lse = -inf.  bf16: where the average sequence fills a tile of 128 rows
- * (tokens x heads of a kv head; pages of 16 or more), the weights are rounded to bf16
- * for the product with the values, as in the whole-prompt attention; otherwise they
- * keep 16 bits and more (within 2^-16), as in the decode step.  H / Hkv <= 128; the block table covers at most 2^30
+ * gives o = 0, lse = -inf.  bf16: where a sequence has more than 64 rows on
+ * average (tokens x heads of a kv head; pages of 16 or more), the weights are rounded to
+ * bf16 for the product with the values, as in the whole-prompt attention; otherwise
+ * they stay within 2^-16.  H / Hkv <= 128; the block table covers at most 2^30
  * positions.  ws: sas_workspace_size(cfg, SAS_OP_ATTENTION_CHUNK, batch, rows),
  * of which all but the last 65 MiB (fewer for dh = 64), where parts of divided
  * work are joined, is needed. */

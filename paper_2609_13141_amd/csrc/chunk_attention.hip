@@ -476,8 +476,8 @@ __device__ __forceinline__ uint2 chunk_read_tr(lds_s16x4_t* __restrict p) {
 
 // One job: a tile's rows over one part of its keys, two tiles of keys in LDS by turns, one
 // barrier a tile.  Bound by the keys' bytes where rows are few: one row over 131000 cached
-// (32/32 heads of 128, 2.1 GB) 359 us, 6.0 TB/s; 32 sequences of 5 new tokens over up to
-// 16000 (28/4 heads, 280 MB) 50 us, 5.6 TB/s, of which 4.7 us pass before the first key.
+// (32/32 heads of 128, 2.1 GB) 363 us, 5.9 TB/s; 32 sequences of 5 new tokens over up to
+// 16000 (28/4 heads, 280 MB) 51 us, 5.5 TB/s, of which 4.7 us pass before the first key.
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   constexpr bool BF = sizeof(T) == 2;
@@ -720,14 +720,15 @@ __device__ __forceinline__ float pair_max(float x) {
 // tile while the vector unit takes this tile's exponentials and sums, then the products
 // with the values; none waits for the other.  K runs a tile ahead of V in LDS: an
 // iteration reads K(t + 1) and V(t) and loads K(t + 2) and V(t + 1), with one barrier.
-// 2048 tokens over 30005 cached, 28/4 heads of 128: 0.885 ms (1.03 PFLOP/s; the plain
-// loop 0.961 ms, a large product reaches 1.4 PFLOP/s); 2304 tokens, whose tiles fill every
-// workgroup, 1.08 PFLOP/s.  What bounds it is the card's power: the clock is at 1.9 GHz
-// of 2.4 (1.8 in a loop of nothing but products), and removing waits alone, 2% of the
-// cycles, took no time off; removing vector instructions did: page lookups in scalar
-// registers (15% of them) 2%, no maxima but where the reference moves 6%.  Not kept: 64
-// keys at a time (181 spilled registers, 3.1 ms), 64 rows a wave with the fragments
-// shared (340).
+// 2048 tokens over 30005 cached, 28/4 heads of 128: 0.90 ms (1.01 PFLOP/s, 0.885 to 0.923
+// from card to card; the plain loop before its second product 0.961 ms, a large product
+// reaches 1.4 PFLOP/s); 2304 tokens, whose tiles fill every workgroup, 1.08 PFLOP/s.  What
+// bounds it: matrix and vector cycles add up (busy in 50% and 40% of all cycles, with 56 of
+// 512 places empty) at a clock of 1.9 GHz of 2.4 (1.8 in a loop of nothing but products).
+// Removing waits alone, 2% of the cycles, took no time off; removing vector instructions
+// did: page lookups in scalar registers (15% of them) 2%, no maxima but where the reference
+// moves 6%.  Not kept: 64 keys at a time (181 spilled registers, 3.1 ms), 64 rows a wave
+// with the fragments shared (340).
 template <int DH>
 __device__ __forceinline__ void chunk_job_piped(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   using T = bf16_t;
@@ -1153,11 +1154,13 @@ hipError_t launch_chunk_attention(int dtype, const ChunkArgs& a, hipStream_t s) 
   const int G = a.H / a.Hkv;
   const int keys = dtype == SAS_BF16 ? ChunkTile<bf16_t>::KEYS : ChunkTile<float>::KEYS;
   const int least = dtype == SAS_BF16 ? ChunkTile<bf16_t>::LEAST : ChunkTile<float>::LEAST;
-  // the pipelined kernel where the average sequence fills a tile: with fewer rows the
-  // keys' bytes bound the call (by it and by the plain loop: 2048 new tokens of 32/32
-  // heads 79.2 and 86.4 us, 4 x 512 of 28/4 heads 32.1 and 33.7; 8 x 1 over 2300 of 32/32
-  // heads 60.7 and 57.4, 32 x 5 over 4000 of 28/4 55.9 and 54.1)
-  const bool piped = dtype == SAS_BF16 && a.ps_shift >= 4 && (long long)a.rows * G > (long long)CHUNK_ROWS * std::min(a.b, a.rows);
+  // the pipelined kernel where the average sequence fills more than half a tile: with fewer
+  // rows the keys' bytes bound the call, and the plain loop's second product hides behind
+  // them.  By it and by the plain loop, us: 32 sequences over 4000 cached, 28/4 heads, of 5
+  // tokens 64.7 and 65.3, of 9 (63 rows) 69.3 and 67.3, of 10 (70 rows) 70.9 and 74.0, of 18
+  // 79.3 and 85.4; 8 over 2000, 32/32 heads, of 1 62.3 and 61.3, of 64 76.0 and 75.9, of 65
+  // 76.4 and 78.0, of 128 106 and 113
+  const bool piped = dtype == SAS_BF16 && a.ps_shift >= 4 && (long long)a.rows * G > (long long)CHUNK_ROWS / 2 * std::min(a.b, a.rows);
   // (tile, kv head) pairs, at most
   const long long tiles = ((long long)a.rows / (CHUNK_ROWS / G) + std::min(a.b, a.rows)) * a.Hkv;
   ChunkKernels k;
