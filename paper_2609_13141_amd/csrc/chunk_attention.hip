@@ -477,7 +477,7 @@ __device__ __forceinline__ uint2 chunk_read_tr(lds_s16x4_t* __restrict p) {
 // One job: a tile's rows over one part of its keys, two tiles of keys in LDS by turns, one
 // barrier a tile.  Bound by the keys' bytes where rows are few: one row over 131000 cached
 // (32/32 heads of 128, 2.1 GB) 363 us, 5.9 TB/s; 32 sequences of 5 new tokens over up to
-// 16000 (28/4 heads, 280 MB) 51 us, 5.5 TB/s, of which 4.7 us pass before the first key.
+// 16000 (28/4 heads, 280 MB) 55 us, 5.1 TB/s, of which 4.7 us pass before the first key.
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, const int rel, const int2 sp) {
   constexpr bool BF = sizeof(T) == 2;
@@ -653,12 +653,12 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
       }
       __builtin_amdgcn_s_setprio(2);
       if constexpr (BF) {
-        // P goes to the matrix unit as two bf16 numbers, the weight's upper half and the rest of
-        // it (together within 2^-16 of the weight), so that a token here is as exact as in the
-        // decode step.  The rest is kept positive (2^-20 of the weight at least): 0, or less
-        // behind a half rounded up, would turn an infinite value into NaN.  The calls of this
-        // loop are bound by the keys' bytes, and the second product nearly hides behind them:
-        // 366 -> 371 us for one row over 131000 cached, 64.5 -> 66.0 for 32 sequences of 5.
+        // P goes to the matrix unit as two bf16 numbers, the upper half of the weight less 2^-20
+        // of it and the rest (together within 2^-16 of the weight), so that a token here is as
+        // exact as in the decode step.  The rest is positive: 0, or less behind a half rounded
+        // up, would turn an infinite value into NaN.  The calls of this loop are bound by the
+        // keys' bytes, and the second product mostly hides behind them: 366 -> 369 us for one
+        // row over 131000 cached, 64.5 -> 65.8 for 32 sequences of 5.
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
           const int st = ks >> 1, v0 = 8 * (ks & 1);
@@ -666,9 +666,9 @@ __device__ __forceinline__ void chunk_job(const ChunkArgs& P, const int seq, con
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float a = s[st][v0 + 2 * j], b = s[st][v0 + 2 * j + 1];
-            const uint32_t a1 = __float_as_uint(a) & 0xffff0000u, b1 = __float_as_uint(b) & 0xffff0000u;
-            hi4[j] = a1 >> 16 | b1;
-            lo4[j] = pack_bf16x2(fmaxf(a - __uint_as_float(a1), a * 0x1p-20f), fmaxf(b - __uint_as_float(b1), b * 0x1p-20f));
+            const uint32_t a1 = __float_as_uint(fmaf(a, -0x1p-20f, a)), b1 = __float_as_uint(fmaf(b, -0x1p-20f, b));
+            hi4[j] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);  // both upper halves
+            lo4[j] = pack_bf16x2(a - __uint_as_float(a1 & 0xffff0000u), b - __uint_as_float(b1 & 0xffff0000u));
           }
           const uint4 pu = make_uint4(hi4[0], hi4[1], hi4[2], hi4[3]), pr = make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]);
           uint4 vu[DH / 32];
