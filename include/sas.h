@@ -641,8 +641,9 @@ typedef struct {
  * y = h1 + SwiGLU(RMSNorm(h1)).  w->w_gq and w->decode_packed are not read.  Padding
  * rows give unspecified outputs.  sas_layer_forward and sas_decode_step know one axis
  * and no head norm: a cache that holds keys with gains, or turned by more than the
- * sequence's positions, is gone on with by this call (single tokens as chunks of one).  ws: sas_workspace_size(cfg, SAS_OP_LAYER_CHUNK,
- * batch, rows); its last part, for partial sums, may be shorter or left out. */
+ * sequence's positions, is gone on with by this call (single tokens as chunks of one).
+ * ws: sas_workspace_size(cfg, SAS_OP_LAYER_CHUNK, batch, rows); its last part, for
+ * partial sums, may be shorter or left out. */
 sas_status sas_layer_chunk(const sas_config* cfg, int32_t batch, int32_t rows, const void* x,
                            const sas_layer_weights* w, const sas_rotary* rot, const sas_chunk* chunk,
                            const sas_paged_kv* cache, void* y, void* ws, size_t ws_bytes, void* stream);

@@ -91,9 +91,9 @@ class Stack:
         [rows] int32, sequence i's new_len[i] after each other at positions
         ctx_len[i] .. (ctx_len, new_len [b] int32, all on the device; rows past
         their sum are padding; tokens past the rows wait for another call, those at
-        positions from max_len on have no page and leave no key).  Returns the last layer's output [rows, d] and
-        the rows' plan (see sas.plan_chunk): kv_len, its lengths after the call, are
-        where the next tokens go."""
+        positions from max_len on have no page and leave no key).  Returns the last
+        layer's output [rows, d] and the rows' plan (see sas.plan_chunk): kv_len, the
+        lengths after the call, are where the next tokens go."""
         x = sas.embed(self.cfg_prefill, ids.view(1, -1), self.ends["embed"])[0]
         none = torch.zeros(1, dtype=torch.int32, device=ids.device)
         plan = None
